@@ -267,6 +267,133 @@ typedef struct {
 LOP_API int lop_plan_rowwise(const lop_rowwise_t* layers, int n_layers, int m, int k, int dtype,
                              int n_bands, unsigned flags, lop_plan_t** out_plan);
 
+/* ---- Operators beside the row-wise products of a transformer ----
+ *
+ * What such a model computes between its matrix products, and those products on 8-bit operands. Every
+ * operator computes a band of rows [rows.lo, rows.hi) of its output from whole inputs, as the chains above do: a
+ * band's rows are final when its kernels are done, and the other rows of the output are left as they were. An empty
+ * band is LOP_OK and enqueues nothing.
+ *
+ * The calls are asynchronous: they enqueue their kernels on `stream` (hipStream_t, NULL = the null stream) of the
+ * current device, on which every pointer and the stream have to be; they allocate nothing, keep nothing between calls, use no other
+ * stream and may be captured into a graph. Everything they are told lies in a descriptor that is read during the call only. Strides
+ * count elements. Pointers that the kernels move 16-byte vectors through start on a 16-byte boundary, and so does every
+ * row and head behind them: strides are multiples of 16 bytes (where the extent is not 1); what is not is
+ * LOP_ERR_INVALID_ARG. Outputs do not overlap inputs unless a comment allows it. */
+
+/* A matrix in 8-bit floating point (e4m3: 3 fraction bits, largest value 448, no infinities) with a scale for each block
+ * of LOP_F8_BLOCK columns: q = x * (448 / a) rounded to nearest even, scale = a / 448, a = max(|x| over the block, 2^-64).
+ * Activations have blocks of one row, weights of LOP_F8_BLOCK rows (block_rows). A NaN stays a NaN and
+ * leaves the rest of its block as it would be without it; an infinity makes the scale infinite, itself NaN and the rest
+ * of its block zero. */
+#define LOP_F8_BLOCK 128
+typedef struct {
+  int m, k;                 /* rows, columns: k a multiple of 16                                          */
+  int dtype;                /* of x: LOP_F32 or LOP_BF16                                                  */
+  int block_rows;           /* 1 or LOP_F8_BLOCK                                                          */
+  const void* x;            /* device                                                                     */
+  long long x_stride;       /* from row to row                                                            */
+  void* q;                  /* device, one byte a value                                                   */
+  long long q_stride;
+  float* scale;             /* device, ceil(m / block_rows) x ceil(k / LOP_F8_BLOCK)                      */
+  long long scale_row, scale_col; /* strides of scale; scale_row == 1 is what lop_rowwise_f8 reads fastest */
+} lop_quantize_t;
+/* rows: of x; with block_rows == LOP_F8_BLOCK lo is a multiple of it, and hi one, or m. */
+LOP_API int lop_quantize_blocks(const lop_quantize_t* op, lop_rows_t rows, void* stream);
+
+/* The row-wise operator (Eq. 1) on operands quantized like that: y = act(x W^T + bias + residual), x of m x k with
+ * blocks of one row, W of n x k (one row per output column) with blocks of LOP_F8_BLOCK rows. The products of a block of columns are summed
+ * by the matrix cores into fp32 (for bf16 outputs by their 8-bit instructions, to about 1.4e-5 of the sum; for fp32 outputs in full), the block's sum is multiplied
+ * by both scales in fp32 and added to that of the blocks before it; y is rounded once. Any m and n; k a multiple of 16. A NaN passes the activation. */
+typedef struct {
+  int m, n, k;
+  int dtype;                /* of residual and y: LOP_F32 or LOP_BF16                                     */
+  int act;                  /* lop_act_t                                                                  */
+  const void* x;            /* device, e4m3                                                               */
+  long long x_stride;
+  const float* x_scale;     /* device, m x ceil(k / LOP_F8_BLOCK)                                         */
+  long long x_scale_row, x_scale_col;
+  const void* w;            /* device, e4m3                                                               */
+  long long w_stride;
+  const float* w_scale;     /* device, ceil(n / LOP_F8_BLOCK) x ceil(k / LOP_F8_BLOCK)                    */
+  long long w_scale_row, w_scale_col;
+  const float* bias;        /* device, n values, or NULL                                                  */
+  const void* residual;     /* device, m x n, or NULL; may be y itself                                    */
+  long long residual_stride;
+  void* y;                  /* device, m x n                                                              */
+  long long y_stride;       /* (y and residual: any alignment of their elements)                          */
+} lop_rowwise_f8_t;
+LOP_API int lop_rowwise_f8(const lop_rowwise_f8_t* op, lop_rows_t rows, void* stream);
+
+/* Queries and keys of every token, each head by itself: x * rsqrt(mean(x^2) + eps) * weight (where a weight is given),
+ * then its first rot_dim values rotated by the token's position in pairs (a, b) -> amplitude * (a cos - b sin, a sin + b cos) with the angle
+ * position * freq[pair]. Pair i is values 2i and 2i + 1 (interleaved) or i and i + rot_dim / 2. A scaling for longer contexts is a matter of the
+ * frequencies and the amplitude that are passed. Angles are formed and reduced in 64 bits, so that far positions keep
+ * theirs; the rest is fp32, each output rounded once. q_out may be q and k_out k, with the same strides. */
+typedef struct {
+  int tokens, heads_q, heads_k; /* heads_k == 0: no keys (k pointers are not read)                        */
+  int head_dim;             /* a multiple of 8, at most 256                                               */
+  int rot_dim;              /* a multiple of 8, 0 .. head_dim                                             */
+  int interleaved;
+  int dtype;                /* LOP_F32 or LOP_BF16                                                        */
+  float eps, amplitude;
+  const void* q;            /* device                                                                     */
+  long long q_token, q_head;
+  const void* k;
+  long long k_token, k_head;
+  void* q_out;
+  long long q_out_token, q_out_head;
+  void* k_out;
+  long long k_out_token, k_out_head;
+  const float* q_weight;    /* device, head_dim values, or NULL: not normalized                           */
+  const float* k_weight;
+  const int* positions;     /* device, one per token                                                      */
+  const float* freq;        /* device, rot_dim / 2 values: radians a position                             */
+} lop_head_norm_rope_t;
+/* rows: tokens. */
+LOP_API int lop_head_norm_rope(const lop_head_norm_rope_t* op, lop_rows_t rows, void* stream);
+
+/* Softmax attention of packed query rows: sequence i's queries are rows q_offsets[i] .. q_offsets[i + 1] of q and out, its keys and values
+ * rows k_begin[i] .. k_end[i] of k and v (packed: k_begin = offsets, k_end = offsets + 1; a cache with room: where each sequence's
+ * part begins and how far it is filled). heads_q / heads_k query heads in a row share a key head. out = softmax(scale q k^T) v over the keys a
+ * row sees: all of its sequence, or (causal) the first nk - nq + r + 1 for row r of nq: the last row sees every key. A row
+ * that sees none is zeros, its lse -infinity. Rows of q before the first or behind the last sequence, and their out and lse, are left as they are. Keys and values
+ * that a row does not see do not touch it, whatever they hold. A local operator in its rows once a sequence's keys are
+ * there: a band needs no other row of q.
+ * Scores, maxima, sums and outputs are held in fp32; with bf16 storage the weights exp(score - maximum) are rounded to bf16 for their product with
+ * v (their sum is taken of the unrounded ones).
+ * The offsets are read on the device; what lies outside 0 .. rows_q or rows_k is cut off there. */
+typedef struct {
+  int dtype;                /* LOP_F32 or LOP_BF16                                                        */
+  int heads_q, heads_k;     /* heads_q a multiple of heads_k                                              */
+  int head_dim;             /* a multiple of 8, at most 256                                               */
+  int seqs;
+  int rows_q, rows_k;       /* rows of q (and out), of k (and v): all that may be touched                 */
+  int max_keys;             /* keys of the longest sequence, as far as known: decides only how the work is cut   */
+  int causal;
+  float scale;              /* finite, above 0                                                            */
+  const void* q;            /* device                                                                     */
+  long long q_token, q_head;
+  const void* k;
+  long long k_token, k_head;
+  const void* v;
+  long long v_token, v_head;
+  void* out;
+  long long out_token, out_head;
+  const int* q_offsets;     /* device, seqs + 1 values, ascending                                         */
+  const int* k_begin;       /* device, seqs values                                                        */
+  const int* k_end;         /* device, seqs values                                                        */
+  float* lse;               /* device, heads_q x rows_q, natural logarithms of the sums of exponentials, or NULL */
+  void* workspace;          /* device, for the partial results of keys cut into parts; may hold anything  */
+  unsigned long long workspace_bytes;
+} lop_attention_t;
+/* Bytes of workspace that lop_attention wants for these sizes and this band (0: none); the workspace, pointers and device values are not
+ * looked at. Given less (or NULL), the call runs without cutting the keys, to the same results up to the order of sums. Calls
+ * whose kernels may overlap need a workspace each. */
+LOP_API int lop_attention_workspace(const lop_attention_t* op, lop_rows_t rows, unsigned long long* bytes);
+/* rows: of q. */
+LOP_API int lop_attention(const lop_attention_t* op, lop_rows_t rows, void* stream);
+
 /* ---- Local-operation scheduling model (Sec. IV-C): host arithmetic only, no GPU ----
  *
  * A vertex's operations are its output rows. A schedule gives every vertex two contiguous

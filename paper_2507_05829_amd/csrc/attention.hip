@@ -1,0 +1,502 @@
+// Softmax attention of packed query rows with shared key heads (lop_attention).
+//
+//   out = sum over j of exp(c s_j - c m) v_j / sum over j of exp(c s_j - c m),   s_j = q . k_j,  m = max s_j,  c = scale
+//
+// in one pass over the keys: maximum, sum and unnormalized output of the keys so far are kept, and multiplied by exp(c m_old - c m_new)
+// where the maximum grows. The query heads that share a key head are rows of one tile, so that its keys and values are read once for all of
+// them, of a prompt as of single tokens.
+//
+// A wavefront holds 32 rows. It computes the scores transposed, keys x rows (k q^T), so that a row is a lane and its
+// mirror image 32 lanes on: a maximum over keys is one over registers and one exchange, and the weights lie as the product with the values
+// (v^T w^T) wants its second operand, whose order of keys is free as long as both operands have the same. Four
+// wavefronts share tiles of KT keys and values, which travel from memory to LDS without passing through registers, one
+// tile ahead.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "conv_common.hpp"
+#include "launch.hpp"
+#include "lop.h"
+#include "op_check.hpp"
+
+namespace lop {
+namespace {
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr unsigned kOut = 0x80000000u;
+constexpr int kRows = 128;            // of a workgroup: 32 for each of four wavefronts
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
+
+struct AttnParams {
+  const char *q, *k, *v;
+  char* out;
+  long long q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;   // bytes
+  const int *q_offsets, *k_begin, *k_end;
+  float* lse;
+  float* part;       // [split][row of q][head][head_dim + 2]: output so far, maximum, sum
+  int heads_k, group, head_dim, seqs, rows_q, rows_k, causal;
+  int lo, hi;        // the band
+  int tile0, tiles;  // of packed rows
+  int splits;
+  float scale;
+};
+
+__device__ __forceinline__ int clamp_to(int v, int most) { return min(max(v, 0), most); }
+
+// Tiles of kRows packed rows (row of the sequence x group + head of the group) are numbered so that sequence i's begin at
+// start(i) = floor(q_offsets[i] group / kRows) + i: at least as many numbers as it has tiles, whatever the lengths, and no list to make.
+struct Place { int seq, tile; };
+__device__ __forceinline__ Place find_tile(const AttnParams& p, int t) {
+  const int lane = threadIdx.x & 63;
+  auto start = [&](int i) { return (int)((long long)clamp_to(p.q_offsets[i], p.rows_q) * p.group / kRows) + i; };
+  int lo = 0, hi = p.seqs;   // the last i with start(i) <= t lies in [lo, hi)
+  while (hi - lo > 1) {
+    const int step = (hi - lo + 63) / 64, i = lo + lane * step;
+    const int n = __popcll(__ballot(i < hi && start(i) <= t));
+    if (n == 0) return Place{-1, 0};   // (only where the first sequence does not begin at row 0)
+    lo += (n - 1) * step;
+    hi = min(hi, lo + step);
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  const int at = t - start(lo);
+  return Place{at < 0 ? -1 : lo, at};
+}
+
+__device__ __forceinline__ float max_of_halves(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __builtin_elementwise_maximum(__uint_as_float((unsigned)s[0]), __uint_as_float((unsigned)s[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float((unsigned)s[0]) + __uint_as_float((unsigned)s[1]);
+}
+
+constexpr int attn_pitch(int bytes) { return bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
+
+// DP: head_dim rounded up to what is computed (a multiple of 32)
+template <typename T, int DP>
+struct AttnShape {
+  static constexpr int E = (int)sizeof(T);
+  static constexpr int PITCH = attn_pitch(DP * E);       // bytes of a key in LDS
+  static constexpr int CP = PITCH / 16;                  // 16-byte chunks of it
+  static constexpr int KT = PITCH <= 512 ? 64 : 32;      // keys of a tile
+  static constexpr int BYTES = KT * PITCH;
+  static constexpr int LDS = 4 * BYTES;                  // two tiles of keys and of values
+  static constexpr int LD = BYTES / 4096;                // load instructions of a wavefront for one tile of either
+  static constexpr int KS = DP * E / 32;                 // operands of a row: steps of 16 bytes in either half
+  static constexpr int DT = DP / 32;
+  // where chunk c of key `row` lies: at c ^ key. Keys: 16 lanes read one chunk of 16 keys. Values: 16 lanes read 32 bytes of four
+  // keys, two such sets side by side (bf16); 32 lanes read 128 bytes of a key and the others of the fourth key on (fp32).
+  static __device__ __forceinline__ int k_key(int row) { return CP == 8 ? (row >> 1) & 7 : row & 15; }
+  static __device__ __forceinline__ int v_key(int row) {
+    if constexpr (E == 4) return ((row >> 2) & 1) * 8;
+    return CP == 8 ? ((row >> 1) & 1) * 4 : (row & 3) * 4;
+  }
+};
+
+// (Where two workgroups fit the LDS of a compute unit their registers have to, too.)
+template <typename T, int DP>
+__global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) void attention_kernel(const AttnParams p) {
+  typedef AttnShape<T, DP> S;
+  constexpr int PITCH = S::PITCH, KT = S::KT, NB = KT / 32, LD = S::LD, KS = S::KS, DT = S::DT, E = S::E;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[S::LDS];
+
+  const int lane = threadIdx.x & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  // The last tiles first: with a causal mask they have the most keys. Key heads fastest: neighbouring workgroups go to different XCDs, whose L2
+  // then holds the keys of one head each where there are eight.
+  const int head = blockIdx.x % p.heads_k;
+  const Place place = find_tile(p, p.tile0 + p.tiles - 1 - blockIdx.x / p.heads_k);
+  if (place.seq < 0) return;
+  const int q0 = clamp_to(p.q_offsets[place.seq], p.rows_q), nq = clamp_to(p.q_offsets[place.seq + 1], p.rows_q) - q0;
+  const int k0 = clamp_to(p.k_begin[place.seq], p.rows_k), nk = max(clamp_to(p.k_end[place.seq], p.rows_k) - k0, 0);
+  const long long packed = (long long)max(nq, 0) * p.group, first = (long long)place.tile * kRows;
+  if (first >= packed) return;
+  const int here = (int)min(packed - first, (long long)kRows);   // rows of this tile
+  // this lane's row
+  const int in_tile = wave * 32 + (lane & 31);
+  const unsigned row = (unsigned)(first + min(in_tile, here - 1));
+  const int token = (int)(row / (unsigned)p.group), qh = head * p.group + (int)(row - (unsigned)token * p.group);
+  const long long at_row = (long long)q0 + token;
+  const bool live = in_tile < here && at_row >= p.lo && at_row < p.hi;
+  // (no row of the tile is in the band)
+  if (q0 + first / p.group >= p.hi || q0 + (first + here - 1) / p.group < p.lo) return;
+  const int sees = p.causal ? min(max(nk - nq + token + 1, 0), nk) : nk;   // keys of this row
+  auto row_sees = [&](int r) {   // of the tile's row r (the same in all lanes)
+    const int t = (int)((first + min(r, here - 1)) / p.group);
+    return p.causal ? min(max(nk - nq + t + 1, 0), nk) : nk;
+  };
+  const bool busy = wave * 32 < here;
+  const int least = row_sees(wave * 32), most = busy ? row_sees(wave * 32 + 31) : 0;
+  const int all = row_sees(kRows - 1);
+  // tiles of keys, and this workgroup's part of them
+  int t0 = 0, t1 = (all + KT - 1) / KT;
+  if (p.splits > 1) {
+    const int each = (t1 + p.splits - 1) / p.splits;
+    t0 = min(blockIdx.y * each, (unsigned)t1);
+    t1 = min(t0 + each, t1);
+  }
+
+  // ---- the rows' operands: 16 bytes at 32 ks + 16 half
+  u32x4 fq[KS];
+  const char* const qp = p.q + at_row * p.q_token + qh * p.q_head;
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    const int at = ks * 32 + half * 16;
+    fq[ks] = u32x4{0u, 0u, 0u, 0u};
+    if (live && at < p.head_dim * E) fq[ks] = *(const u32x4*)(qp + at);
+  }
+
+  // ---- what this lane fetches of a tile
+  unsigned k_off[LD], v_off[LD];
+#pragma unroll
+  for (int i = 0; i < LD; ++i) {
+    const int at = (wave + 4 * i) * 1024 + lane * 16, r = at / PITCH, c = at % PITCH / 16;
+    const int ck = c ^ S::k_key(r), cv = c ^ S::v_key(r);
+    k_off[i] = ck * 16 < p.head_dim * E ? (unsigned)(r * (int)p.k_token + ck * 16) : kOut;
+    v_off[i] = cv * 16 < p.head_dim * E ? (unsigned)(r * (int)p.v_token + cv * 16) : kOut;
+  }
+  const char* const kp = p.k + (long long)k0 * p.k_token + head * p.k_head;
+  const char* const vp = p.v + (long long)k0 * p.v_token + head * p.v_head;
+  auto issue = [&](int t, int buf) __attribute__((always_inline)) {   // (keys past the sequence's last arrive as zeros)
+    const int left = min(nk - t * KT, KT) - 1;
+    const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kp + (long long)t * KT * p.k_token), 0,
+                                                                        left * (int)p.k_token + p.head_dim * E, 0x00020000);
+    const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp + (long long)t * KT * p.v_token), 0,
+                                                                        left * (int)p.v_token + p.head_dim * E, 0x00020000);
+    unsigned char* const dst = smem + buf * 2 * S::BYTES + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(kb, (__attribute__((address_space(3))) void*)(dst + i * 4096), 16, (int)k_off[i], 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < LD; ++i)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(vb, (__attribute__((address_space(3))) void*)(dst + S::BYTES + i * 4096), 16, (int)v_off[i], 0, 0, 0);
+  };
+  auto barrier = [&]() __attribute__((always_inline)) {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  // ---- where it reads: chunk 2 ks + half of key lane mod 32; of the values what the operand v^T wants
+  const unsigned lds0 = (unsigned)(unsigned long)(__attribute__((address_space(3))) unsigned char*)smem;
+  const unsigned k_at = lds0 + (lane & 31) * PITCH + ((half ^ S::k_key(lane & 31)) * 16);
+  unsigned v_at;
+  if constexpr (E == 2) {
+    const int s = lane & 15, key = 4 * half + s / 4;   // (of 16 lanes, see transposed reads below)
+    v_at = lds0 + S::BYTES + key * PITCH + ((2 * ((lane >> 4) & 1) + (s & 3) / 2) ^ S::v_key(key)) * 16 + (s & 1) * 8;
+  } else {
+    const int key = 4 * half;
+    v_at = lds0 + S::BYTES + key * PITCH + (((lane & 31) / 4) ^ S::v_key(key)) * 16 + (lane & 3) * 4;
+  }
+
+  const float c = p.scale * kLog2e;
+  f32x16 o[DT];
+  float m, l;   // maximum of c s, in powers of two; sum
+  // Weights of zero times an infinity or a NaN of a value that the row does not see are NaNs. They are rare, and looked for at the end only: then the
+  // keys are gone through again, those of tiles that some row sees in part one by one.
+  for (int careful = 0; careful < 2; ++careful) {
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    if (t0 < t1) issue(t0, 0);
+    for (int t = t0; t < t1; ++t) {
+      __builtin_amdgcn_s_waitcnt(vmcnt_imm(0));
+      barrier();
+      if (t + 1 < t1) issue(t + 1, (t + 1 - t0) & 1);
+      if (t * KT >= most) continue;
+      const unsigned buf = (unsigned)(((t - t0) & 1) * 2 * S::BYTES);
+      // scores
+      f32x16 s[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+        constexpr int G = KS % 8 == 0 ? 8 : KS;   // reads in flight
+#pragma unroll
+        for (int k0 = 0; k0 < KS; k0 += G) {
+          u32x4 fk[G];
+#pragma unroll
+          for (int i = 0; i < G; ++i)
+            asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(fk[i]) : "v"((k_at + buf) ^ (unsigned)((k0 + i) * 32)), "n"(b * 32 * PITCH) : "memory");
+          unroll<G>([&](auto i) __attribute__((always_inline)) {
+            asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(fk[i]) : "n"(G - 1 - i) : "memory");
+            mma<T>(fk[i], fq[k0 + i], s[b]);
+          });
+        }
+      }
+      const bool partly = t * KT + KT > least;
+      if (partly) {
+        const int upto = sees - t * KT - 4 * half;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[b][i] = b * 32 + (i / 4) * 8 + i % 4 < upto ? s[b][i] : -INFINITY;
+      }
+      // maximum
+      float top = s[0][0];
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = b ? 0 : 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[b][i]);
+      const float grown = __builtin_elementwise_maximum(m, max_of_halves(top) * c);
+      if (__any(grown != m)) {
+        const float by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
+        m = grown;
+        l *= by;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] *= by;
+      }
+      const float from = m == -INFINITY ? 0.f : m;   // (no key so far)
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -from));
+          l += s[b][i];
+        }
+      // output
+      if (careful && partly) {
+        const int upto = sees - t * KT;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll 1
+          for (int i = 0; i < 16; ++i) {
+            const float mine = (float)(T)s[b][i], other = __shfl_xor(mine, 32, 64);
+#pragma unroll 1
+            for (int h = 0; h < 2; ++h) {
+              const int key = b * 32 + (i / 4) * 8 + h * 4 + i % 4;
+              const float w = half == h ? mine : other;
+              const unsigned char* const vrow = smem + buf + S::BYTES + key * PITCH;
+#pragma unroll
+              for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                  const int at = (d * 32 + j * 8 + half * 4) * E;
+                  const T* const x = (const T*)(vrow + (((at / 16) ^ S::v_key(key)) * 16) + at % 16);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) {
+                    const float sum = fmaf(w, to_f32(x[e]), o[d][j * 4 + e]);
+                    o[d][j * 4 + e] = key < upto ? sum : o[d][j * 4 + e];
+                  }
+                }
+            }
+          }
+        continue;
+      }
+      if constexpr (E == 2) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {   // 16 keys: the operand's eight of a lane are keys 4 half + {0..3} and 8 on of them
+            alignas(16) __bf16 w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = (__bf16)s[b][h * 8 + i];
+            const u32x4 fw = *(const u32x4*)w;
+            // Of 16 lanes, lane i gets value i % 4 of the four that lanes i / 4, i / 4 + 4, + 8 and + 12 point at: four keys of one of 16 columns.
+            constexpr int G = DT < 4 ? DT : 4;
+#pragma unroll
+            for (int d0 = 0; d0 < DT; d0 += G) {
+              u32x2 fv[G][2];
+#pragma unroll
+              for (int d = 0; d < G; ++d) {
+                const unsigned at = (v_at + buf) ^ (unsigned)((d0 + d) * 64);
+                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(fv[d][0]) : "v"(at), "n"((b * 32 + h * 16) * PITCH) : "memory");
+                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(fv[d][1]) : "v"(at), "n"((b * 32 + h * 16 + 8) * PITCH) : "memory");
+              }
+              unroll<G>([&](auto d) __attribute__((always_inline)) {
+                asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(fv[d][0]), "+v"(fv[d][1]) : "n"(2 * (G - 1 - d)) : "memory");
+                mma<T>(u32x4{fv[d][0][0], fv[d][0][1], fv[d][1][0], fv[d][1][1]}, fw, o[d0 + d]);
+              });
+            }
+          }
+      } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {   // two keys: one of either half
+            float fv[DT];
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+              asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(fv[d]) : "v"((v_at + buf) ^ (unsigned)(d * 128)), "n"((b * 32 + (i / 4) * 8 + i % 4) * PITCH) : "memory");
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+            for (int d = 0; d < DT; ++d) asm volatile("" : "+v"(fv[d]));
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(fv[d], s[b][i], o[d], 0, 0, 0);
+          }
+      }
+    }
+    bool odd = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd |= live && !(fabsf(o[d][i]) < INFINITY);
+    if (careful || !__syncthreads_or(odd)) break;
+  }
+  l = sum_of_halves(l);
+  if (!live) return;
+
+  if (p.splits > 1) {
+    const long long slot = ((long long)blockIdx.y * (p.hi - p.lo) + at_row - p.lo) * (p.heads_k * p.group) + qh;
+    float* const to = p.part + slot * (p.head_dim + 2);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int at = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
+        if (at < p.head_dim) to[at] = o[d][i];
+      }
+    if (half == 0) { to[p.head_dim] = m; to[p.head_dim + 1] = sees > 0 ? l : -1.f; }
+    return;
+  }
+  const float by = sees > 0 ? 1.f / l : 0.f;
+  char* const op = p.out + at_row * p.out_token + qh * p.out_head;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int at = d * 32 + j * 8 + half * 4;
+      if (at >= p.head_dim) continue;
+      alignas(16) T w[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(sees > 0 ? o[d][j * 4 + e] * by : 0.f);
+      __builtin_memcpy(__builtin_assume_aligned(op + at * E, 4 * E), w, sizeof(w));
+    }
+  if (p.lse && half == 0) p.lse[(long long)qh * p.rows_q + at_row] = sees > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
+}
+
+// Joins the parts of a row: a wavefront for each row and head. (A sum of -1: the row sees no key.)
+template <typename T>
+__global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p) {
+  const int lane = threadIdx.x & 63, heads = p.heads_k * p.group;
+  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int head = (int)(at % heads);
+  const long long row = p.lo + at / heads;
+  const int first = clamp_to(p.q_offsets[0], p.rows_q), last = clamp_to(p.q_offsets[p.seqs], p.rows_q);
+  if (row >= p.hi || row < first || row >= last) return;
+  const long long pitch = p.head_dim + 2, step = (long long)(p.hi - p.lo) * heads * pitch;
+  const float* const parts = p.part + at * pitch;
+  float m = -INFINITY;
+  for (int s = 0; s < p.splits; ++s) m = __builtin_elementwise_maximum(m, parts[s * step + p.head_dim]);
+  const float from = m == -INFINITY ? 0.f : m;
+  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+  const bool here = lane * 4 < p.head_dim;
+  for (int s = 0; s < p.splits; ++s) {
+    const float* const x = parts + s * step;
+    const float by = __builtin_amdgcn_exp2f(x[p.head_dim] - from);
+    l = fmaf(by, x[p.head_dim + 1], l);
+    if (here)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = fmaf(by, x[lane * 4 + i], o[i]);
+  }
+  const bool none = parts[p.head_dim + 1] < 0.f;
+  if (here) {
+    alignas(16) T w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = from_f32<T>(none ? 0.f : o[i] / l);
+    __builtin_memcpy(__builtin_assume_aligned(p.out + row * p.out_token + head * p.out_head + lane * 4 * (int)sizeof(T), 4 * sizeof(T)), w, sizeof(w));
+  }
+  if (p.lse && lane == 0) p.lse[(long long)head * p.rows_q + row] = none ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// Tiles whose numbers the rows of a band can have (see find_tile: a row's lies between floor(row group / kRows) - 1 and floor(...) + its sequence).
+struct Cut { int tile0, tiles, splits; };
+Cut cut(const lop_attention_t* op, lop_rows_t rows) {
+  const long long group = op->heads_q / op->heads_k;
+  Cut c;
+  c.tile0 = (int)std::max(rows.lo * group / kRows - 1, 0LL);
+  c.tiles = (int)((rows.hi * group - 1) / kRows + op->seqs - c.tile0);
+  // Two workgroups fit a compute unit. Where there are fewer than that the keys are cut into parts of 256 at least.
+  const long long blocks = (long long)c.tiles * op->heads_k;
+  c.splits = (int)std::max(1LL, std::min({ceil_div(1024, blocks), (long long)std::max(op->max_keys, 1) / 256, 64LL}));
+  if (blocks >= 512) c.splits = 1;
+  return c;
+}
+unsigned long long workspace_of(const lop_attention_t* op, lop_rows_t rows, int splits) {
+  return splits < 2 ? 0 : (unsigned long long)splits * (rows.hi - rows.lo) * op->heads_q * (op->head_dim + 2) * sizeof(float);
+}
+
+int check_sizes(const lop_attention_t* op, lop_rows_t rows) {
+  if (!op || op->heads_q < 1 || op->heads_k < 1 || op->head_dim < 1 || op->seqs < 0 || op->rows_q < 0 || op->rows_k < 0 || op->max_keys < 0)
+    return LOP_ERR_INVALID_ARG;
+  if (!known_dtype(op->dtype) || op->head_dim % 8 || op->head_dim > 256) return LOP_ERR_UNSUPPORTED;
+  if (op->heads_q % op->heads_k) return LOP_ERR_SHAPE;
+  if (const int e = check_band(rows, op->rows_q)) return e;
+  const long long group = op->heads_q / op->heads_k, packed = (long long)op->rows_q * group;
+  if (packed >= (1LL << 31) || (packed / kRows + op->seqs + 1) * op->heads_k > launch_blocks(256) ||
+      ceil_div((long long)op->rows_q * op->heads_q, 4) > launch_blocks(256))
+    return LOP_ERR_UNSUPPORTED;
+  return LOP_OK;
+}
+
+template <typename T>
+hipError_t launch_attention(const AttnParams& p, hipStream_t s) {
+  const dim3 grid((unsigned)p.tiles * (unsigned)p.heads_k, (unsigned)p.splits), block(256);
+  const hipError_t e = p.head_dim <= 64    ? launch_kernel(attention_kernel<T, 64>, grid, block, s, nullptr, p)
+                       : p.head_dim <= 96  ? launch_kernel(attention_kernel<T, 96>, grid, block, s, nullptr, p)
+                       : p.head_dim <= 128 ? launch_kernel(attention_kernel<T, 128>, grid, block, s, nullptr, p)
+                                           : launch_kernel(attention_kernel<T, 256>, grid, block, s, nullptr, p);
+  if (e != hipSuccess || p.splits < 2) return e;
+  const long long waves = (long long)(p.hi - p.lo) * p.heads_k * p.group;
+  return launch_kernel(attention_join_kernel<T>, dim3((unsigned)ceil_div(waves, 4)), block, s, nullptr, p);
+}
+
+}  // namespace
+}  // namespace lop
+
+extern "C" int lop_attention_workspace(const lop_attention_t* op, lop_rows_t rows, unsigned long long* bytes) {
+  using namespace lop;
+  if (!bytes) return LOP_ERR_INVALID_ARG;
+  *bytes = 0;
+  if (const int e = check_sizes(op, rows)) return e;
+  if (rows.lo < rows.hi && op->seqs > 0) *bytes = workspace_of(op, rows, cut(op, rows).splits);
+  return LOP_OK;
+}
+
+extern "C" int lop_attention(const lop_attention_t* op, lop_rows_t rows, void* stream) {
+  using namespace lop;
+  if (const int e = check_sizes(op, rows)) return e;
+  if (!(op->scale > 0.f) || !(op->scale < INFINITY)) return LOP_ERR_INVALID_ARG;
+  if (rows.lo == rows.hi || op->seqs == 0) return LOP_OK;
+  const long long E = (long long)dtype_bytes(op->dtype);
+  auto good = [&](const void* p, long long token, long long head, int rows_of, int heads) {
+    return p && aligned16(p) && whole_vectors(token, E, rows_of > 1) && whole_vectors(head, E, heads > 1);
+  };
+  if (!good(op->q, op->q_token, op->q_head, op->rows_q, op->heads_q) || !good(op->out, op->out_token, op->out_head, op->rows_q, op->heads_q))
+    return LOP_ERR_INVALID_ARG;
+  if (op->rows_k > 0 && (!good(op->k, op->k_token, op->k_head, op->rows_k, op->heads_k) || !good(op->v, op->v_token, op->v_head, op->rows_k, op->heads_k)))
+    return LOP_ERR_INVALID_ARG;
+  if (!op->q_offsets || !op->k_begin || !op->k_end) return LOP_ERR_INVALID_ARG;
+  if (((uintptr_t)op->q_offsets | (uintptr_t)op->k_begin | (uintptr_t)op->k_end | (uintptr_t)op->lse | (uintptr_t)op->workspace) & 3) return LOP_ERR_INVALID_ARG;
+  // (a tile's keys are one buffer: its rows lie behind one another, and offsets in it are 32 bits)
+  if (op->rows_k > 1 && (op->k_token < op->head_dim || op->v_token < op->head_dim)) return LOP_ERR_INVALID_ARG;
+  if (op->rows_k > 1 && (op->k_token * E > (1LL << 31) / 128 || op->v_token * E > (1LL << 31) / 128)) return LOP_ERR_UNSUPPORTED;
+  const Cut c = cut(op, rows);
+  AttnParams p;
+  p.q = (const char*)op->q; p.k = (const char*)op->k; p.v = (const char*)op->v; p.out = (char*)op->out;
+  p.q_token = op->q_token * E; p.q_head = op->q_head * E; p.out_token = op->out_token * E; p.out_head = op->out_head * E;
+  p.k_token = op->rows_k > 1 ? op->k_token * E : 0; p.k_head = op->k_head * E;
+  p.v_token = op->rows_k > 1 ? op->v_token * E : 0; p.v_head = op->v_head * E;
+  p.q_offsets = op->q_offsets; p.k_begin = op->k_begin; p.k_end = op->k_end;
+  p.lse = op->lse;
+  p.heads_k = op->heads_k; p.group = op->heads_q / op->heads_k; p.head_dim = op->head_dim;
+  p.seqs = op->seqs; p.rows_q = op->rows_q; p.rows_k = op->rows_k; p.causal = op->causal != 0;
+  p.lo = rows.lo; p.hi = rows.hi;
+  p.tile0 = c.tile0; p.tiles = c.tiles;
+  p.splits = c.splits > 1 && op->workspace && op->workspace_bytes >= workspace_of(op, rows, c.splits) ? c.splits : 1;
+  p.part = (float*)op->workspace;
+  p.scale = op->scale;
+  LOP_HIP(op->dtype == LOP_BF16 ? launch_attention<__bf16>(p, (hipStream_t)stream) : launch_attention<float>(p, (hipStream_t)stream));
+  return LOP_OK;
+}

@@ -1,0 +1,27 @@
+// What the operators beside the row-wise products check of their arguments, on the host, before anything is enqueued.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "lop.h"
+#include "plan_state.hpp"
+
+namespace lop {
+
+inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+// A tensor that 16-byte vectors are moved through: non-null, on a 16-byte boundary, as is whatever a stride leads to (`used`: the
+// extent is more than 1). Strides are not negative: the kernels' offsets are not.
+inline bool whole_vectors(long long stride, size_t element, bool used) {
+  return !used || (stride >= 0 && (size_t)stride * element % 16 == 0);
+}
+inline size_t dtype_bytes(int dtype) { return dtype == LOP_BF16 ? 2 : 4; }
+inline bool known_dtype(int dtype) { return dtype == LOP_F32 || dtype == LOP_BF16; }
+// LOP_OK, or what a band that is no interval of `total` rows is
+inline int check_band(lop_rows_t r, long long total) { return r.lo < 0 || r.hi < r.lo || r.hi > total ? LOP_ERR_BAND_RANGE : LOP_OK; }
+// Workgroups of one dimension that a launch takes: fewer than 2^32 threads (exclusive).
+constexpr long long launch_blocks(int threads) { return 0xffffffffLL / threads; }
+constexpr long long ceil_div(long long a, long long b) { return (a + b - 1) / b; }
+
+}  // namespace lop

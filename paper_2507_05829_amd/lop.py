@@ -11,7 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_size_t, c_uint, c_void_p
+from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_longlong, c_size_t, c_uint, c_ulonglong, c_void_p
 from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -39,6 +39,7 @@ LOP_FLAG_NO_FUSE = 32
 LOP_FLAG_POISON_SCRATCH = 64
 LOP_FLAG_BATCH_BANDS = 128
 LOP_LINK_INDEPENDENT, LOP_LINK_QUEUED = 0, 1
+LOP_F8_BLOCK = 128
 
 
 def LOP_FLAG_LANES(n: int) -> int:
@@ -53,6 +54,7 @@ EXPORTS = [
     "lop_last_hip_error", "lop_plan_layer_kernel", "lop_profile_chain", "lop_copy_chain",
     "lop_plan_band_compute_rows", "lop_plan_rowwise", "lop_loss_eval", "lop_loss_solve",
     "lop_run_two_party", "lop_measure_ceilings", "lop_run_chain_static", "lop_debug_guard_check",
+    "lop_quantize_blocks", "lop_rowwise_f8", "lop_head_norm_rope", "lop_attention_workspace", "lop_attention",
 ]
 
 
@@ -88,6 +90,45 @@ class lop_two_party_stats_t(Structure):
 class lop_ceilings_t(Structure):
     _fields_ = [("hbm_copy_gbs", c_double), ("mfma_bf16_tflops", c_double), ("mfma_f32_tflops", c_double),
                 ("launch_floor_us", c_double), ("graph_node_floor_us", c_double)]
+
+
+class lop_quantize_t(Structure):
+    _fields_ = [("m", c_int), ("k", c_int), ("dtype", c_int), ("block_rows", c_int),
+                ("x", c_void_p), ("x_stride", c_longlong), ("q", c_void_p), ("q_stride", c_longlong),
+                ("scale", c_void_p), ("scale_row", c_longlong), ("scale_col", c_longlong)]
+
+
+class lop_rowwise_f8_t(Structure):
+    _fields_ = [("m", c_int), ("n", c_int), ("k", c_int), ("dtype", c_int), ("act", c_int),
+                ("x", c_void_p), ("x_stride", c_longlong),
+                ("x_scale", c_void_p), ("x_scale_row", c_longlong), ("x_scale_col", c_longlong),
+                ("w", c_void_p), ("w_stride", c_longlong),
+                ("w_scale", c_void_p), ("w_scale_row", c_longlong), ("w_scale_col", c_longlong),
+                ("bias", c_void_p), ("residual", c_void_p), ("residual_stride", c_longlong),
+                ("y", c_void_p), ("y_stride", c_longlong)]
+
+
+class lop_head_norm_rope_t(Structure):
+    _fields_ = [("tokens", c_int), ("heads_q", c_int), ("heads_k", c_int), ("head_dim", c_int),
+                ("rot_dim", c_int), ("interleaved", c_int), ("dtype", c_int),
+                ("eps", c_float), ("amplitude", c_float),
+                ("q", c_void_p), ("q_token", c_longlong), ("q_head", c_longlong),
+                ("k", c_void_p), ("k_token", c_longlong), ("k_head", c_longlong),
+                ("q_out", c_void_p), ("q_out_token", c_longlong), ("q_out_head", c_longlong),
+                ("k_out", c_void_p), ("k_out_token", c_longlong), ("k_out_head", c_longlong),
+                ("q_weight", c_void_p), ("k_weight", c_void_p), ("positions", c_void_p), ("freq", c_void_p)]
+
+
+class lop_attention_t(Structure):
+    _fields_ = [("dtype", c_int), ("heads_q", c_int), ("heads_k", c_int), ("head_dim", c_int),
+                ("seqs", c_int), ("rows_q", c_int), ("rows_k", c_int), ("max_keys", c_int),
+                ("causal", c_int), ("scale", c_float),
+                ("q", c_void_p), ("q_token", c_longlong), ("q_head", c_longlong),
+                ("k", c_void_p), ("k_token", c_longlong), ("k_head", c_longlong),
+                ("v", c_void_p), ("v_token", c_longlong), ("v_head", c_longlong),
+                ("out", c_void_p), ("out_token", c_longlong), ("out_head", c_longlong),
+                ("q_offsets", c_void_p), ("k_begin", c_void_p), ("k_end", c_void_p), ("lse", c_void_p),
+                ("workspace", c_void_p), ("workspace_bytes", c_ulonglong)]
 
 
 class lop_tensor_desc_t(Structure):
@@ -146,6 +187,11 @@ def _load() -> ctypes.CDLL:
                                       POINTER(lop_loss_layer_t), c_double, c_double,
                                       POINTER(lop_two_party_stats_t)]),
         "lop_measure_ceilings": (c_int, [POINTER(lop_ceilings_t)]),
+        "lop_quantize_blocks": (c_int, [POINTER(lop_quantize_t), lop_rows_t, c_void_p]),
+        "lop_rowwise_f8": (c_int, [POINTER(lop_rowwise_f8_t), lop_rows_t, c_void_p]),
+        "lop_head_norm_rope": (c_int, [POINTER(lop_head_norm_rope_t), lop_rows_t, c_void_p]),
+        "lop_attention_workspace": (c_int, [POINTER(lop_attention_t), lop_rows_t, POINTER(c_ulonglong)]),
+        "lop_attention": (c_int, [POINTER(lop_attention_t), lop_rows_t, c_void_p]),
         "lop_debug_guard_check": (c_int, []),
         "lop_strerror": (c_char_p, [c_int]),
         "lop_last_hip_error": (c_int, []),
@@ -370,6 +416,28 @@ def lop_measure_ceilings() -> lop_ceilings_t:
     return c
 
 
+def lop_quantize_blocks(op: lop_quantize_t, rows: Tuple[int, int], stream=None) -> None:
+    _check(_lib.lop_quantize_blocks(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_quantize_blocks")
+
+
+def lop_rowwise_f8(op: lop_rowwise_f8_t, rows: Tuple[int, int], stream=None) -> None:
+    _check(_lib.lop_rowwise_f8(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_rowwise_f8")
+
+
+def lop_head_norm_rope(op: lop_head_norm_rope_t, rows: Tuple[int, int], stream=None) -> None:
+    _check(_lib.lop_head_norm_rope(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_head_norm_rope")
+
+
+def lop_attention_workspace(op: lop_attention_t, rows: Tuple[int, int]) -> int:
+    n = c_ulonglong(0)
+    _check(_lib.lop_attention_workspace(byref(op), lop_rows_t(*rows), byref(n)), "lop_attention_workspace")
+    return n.value
+
+
+def lop_attention(op: lop_attention_t, rows: Tuple[int, int], stream=None) -> None:
+    _check(_lib.lop_attention(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_attention")
+
+
 def lop_debug_guard_check() -> int:
     return _lib.lop_debug_guard_check()
 
@@ -507,3 +575,178 @@ class Plan:
 
     def time_layer(self, band, layer, d_in, d_out, iters=20):
         return lop_time_layer(self.handle, band, layer, d_in, d_out, iters)
+
+
+# ------------------------------------------------------------------ operators on torch tensors
+#
+# lop_quantize_blocks, lop_rowwise_f8, lop_head_norm_rope and lop_attention on tensors: the descriptor is read off
+# them. They run on torch's current stream of the current device, where every tensor has to be; outputs that are not
+# passed are allocated there. `rows`: the band of output rows that is computed (lo, hi), everything if None. Forward
+# only: a tensor that wants a gradient is refused while gradients are recorded. Shapes and types that do not fit
+# raise ValueError, what the library refuses LopError.
+
+# (the library's host code also runs beside a stand-in for torch that has no tensors)
+_TYPES = {getattr(torch, n): c for n, c in (("float32", LOP_F32), ("bfloat16", LOP_BF16)) if hasattr(torch, n)}
+_F8 = getattr(torch, "float8_e4m3fn", None)
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def _tensors(*named) -> int:
+    """Checks that (name, tensor, dimensions, type) are tensors of the current device; None is passed over. Returns the
+    current stream."""
+    device = torch.cuda.current_device()
+    grad = torch.is_grad_enabled()
+    for name, t, dims, dtype in named:
+        if t is None:
+            continue
+        if t.dim() != dims or t.dtype != dtype:
+            raise ValueError(f"{name}: {dims} dimensions of {dtype} are wanted, not {t.dim()} of {t.dtype}")
+        if not t.is_cuda or t.get_device() != device:
+            raise ValueError(f"{name}: on {t.device}, not on the current device ({device})")
+        if grad and t.requires_grad:
+            raise ValueError(f"{name}: forward only, but the tensor wants a gradient")
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _dtype(name: str, t: torch.Tensor) -> int:
+    code = _TYPES.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name}: float32 or bfloat16 is wanted, not {t.dtype}")
+    return code
+
+
+def _inner(name: str, t) -> None:
+    if t is not None and t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel() > 0:
+        raise ValueError(f"{name}: the values of a row have to lie next to one another")
+
+
+def _at(t):
+    return None if t is None else t.data_ptr()
+
+
+def _band(rows, total: int) -> lop_rows_t:
+    return lop_rows_t(0, total) if rows is None else lop_rows_t(*rows)
+
+
+def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
+    """x (m, k) in e4m3 with a scale for each block of `block_rows` x 128 values (see lop_quantize_blocks). Returns
+    (q, scale): q float8_e4m3fn (m, k), scale float32 (ceil(m / block_rows), ceil(k / 128)), allocated with the scales
+    of a column of blocks next to one another."""
+    dtype = _dtype("x", x)
+    stream = _tensors(("x", x, 2, x.dtype), ("q", q, 2, _F8), ("scale", scale, 2, torch.float32))
+    m, k = x.shape
+    _need(block_rows in (1, LOP_F8_BLOCK), f"block_rows: 1 or {LOP_F8_BLOCK}")
+    shape = (-(-m // block_rows), -(-k // LOP_F8_BLOCK))
+    if q is None:
+        q = torch.empty((m, k), dtype=_F8, device=x.device)
+    if scale is None:
+        scale = torch.empty(shape[::-1], dtype=torch.float32, device=x.device).t()
+    _need(q.shape == x.shape and scale.shape == shape, f"q is {tuple(x.shape)} and scale {shape}")
+    _inner("x", x)
+    _inner("q", q)
+    op = lop_quantize_t(m, k, dtype, block_rows, x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0), scale.data_ptr(),
+                        scale.stride(0), scale.stride(1))
+    _check(_lib.lop_quantize_blocks(byref(op), _band(rows, m), stream), "lop_quantize_blocks")
+    return q, scale
+
+
+def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=None, y=None, dtype=None, rows=None):
+    """act(x W^T + bias + residual) of operands quantized by quantize_blocks: x (m, k) with blocks of one row, w (n, k)
+    with blocks of 128 rows (see lop_rowwise_f8). y (m, n) is allocated in `dtype` (None: bfloat16) if it is not passed."""
+    dtype = y.dtype if y is not None else dtype or torch.bfloat16
+    _need(dtype in _TYPES, "y: float32 or bfloat16")
+    _need(act in _ACTS, f"act: one of {sorted(_ACTS)}")
+    f32 = torch.float32
+    stream = _tensors(("x", x, 2, _F8), ("x_scale", x_scale, 2, f32), ("w", w, 2, _F8), ("w_scale", w_scale, 2, f32),
+                      ("bias", bias, 1, f32), ("residual", residual, 2, dtype), ("y", y, 2, dtype))
+    m, k = x.shape
+    n, kb = w.shape[0], -(-k // LOP_F8_BLOCK)
+    if y is None:
+        y = torch.empty((m, n), dtype=dtype, device=x.device)
+    _need(w.shape[1] == k, "x and w have different numbers of columns")
+    _need(x_scale.shape == (m, kb) and w_scale.shape == (-(-n // LOP_F8_BLOCK), kb), "scales do not fit their matrices")
+    _need(y.shape == (m, n) and (residual is None or residual.shape == (m, n)) and (bias is None or bias.shape == (n,)),
+          f"y and residual are {(m, n)}, bias {(n,)}")
+    for name, t in (("x", x), ("w", w), ("bias", bias), ("residual", residual), ("y", y)):
+        _inner(name, t)
+    op = lop_rowwise_f8_t(m, n, k, _TYPES[dtype], _ACTS[act], x.data_ptr(), x.stride(0), x_scale.data_ptr(), x_scale.stride(0),
+                          x_scale.stride(1), w.data_ptr(), w.stride(0), w_scale.data_ptr(), w_scale.stride(0), w_scale.stride(1),
+                          _at(bias), _at(residual), 0 if residual is None else residual.stride(0), y.data_ptr(), y.stride(0))
+    _check(_lib.lop_rowwise_f8(byref(op), _band(rows, m), stream), "lop_rowwise_f8")
+    return y
+
+
+def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+                   amplitude: float = 1.0, q_out=None, k_out=None, rows=None):
+    """q (tokens, heads_q, d) and k (tokens, heads_k, d) or None, each head normalized (where its weight (d,) is given) and its first
+    2 * len(freq) values rotated by positions * freq (see lop_head_norm_rope). positions int32 (tokens,), freq float32,
+    both None for no rotation. Returns (q_out, k_out), which may be q and k."""
+    dtype = _dtype("q", q)
+    f32 = torch.float32
+    stream = _tensors(("q", q, 3, q.dtype), ("k", k, 3, q.dtype), ("positions", positions, 1, torch.int32), ("freq", freq, 1, f32),
+                      ("q_weight", q_weight, 1, f32), ("k_weight", k_weight, 1, f32), ("q_out", q_out, 3, q.dtype),
+                      ("k_out", k_out, 3, q.dtype))
+    tokens, hq, d = q.shape
+    hk = 0 if k is None else k.shape[1]
+    if q_out is None:
+        q_out = torch.empty((tokens, hq, d), dtype=q.dtype, device=q.device)
+    if k_out is None and k is not None:
+        k_out = torch.empty((tokens, hk, d), dtype=q.dtype, device=q.device)
+    _need(k is None or k.shape == (tokens, hk, d), "q and k have different tokens or head sizes")
+    _need(q_out.shape == q.shape and (k is None or k_out.shape == k.shape), "outputs have their inputs' shapes")
+    _need((positions is None) == (freq is None), "positions and freq go together")
+    _need(positions is None or positions.shape == (tokens,), "a position for each token")
+    for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
+        _need(t is None or t.shape == (d,), f"{name}: a value for each of a head's")
+    for name, t in (("q", q), ("k", k), ("positions", positions), ("freq", freq), ("q_weight", q_weight), ("k_weight", k_weight),
+                    ("q_out", q_out), ("k_out", k_out)):
+        _inner(name, t)
+    ks, kos = (0, 0, 0) if k is None else k.stride(), (0, 0, 0) if k is None else k_out.stride()
+    qs, qos = q.stride(), q_out.stride()
+    op = lop_head_norm_rope_t(tokens, hq, hk, d, 0 if freq is None else 2 * freq.shape[0], int(interleaved), dtype, eps, amplitude,
+                              q.data_ptr(), qs[0], qs[1], _at(k), ks[0], ks[1], q_out.data_ptr(), qos[0], qos[1],
+                              _at(k_out), kos[0], kos[1], _at(q_weight), _at(k_weight), _at(positions), _at(freq))
+    _check(_lib.lop_head_norm_rope(byref(op), _band(rows, tokens), stream), "lop_head_norm_rope")
+    return q_out, k_out
+
+
+def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = True, max_keys: Optional[int] = None, out=None, lse=None,
+              workspace=None, rows=None):
+    """softmax(scale q k^T) v of packed sequences (see lop_attention): q (rows_q, heads_q, d), k and v (rows_k, heads_k, d); sequence
+    i's queries are rows q_offsets[i] .. q_offsets[i + 1], its keys rows k_begin[i] .. k_end[i] (int32 tensors). max_keys: keys of the longest
+    sequence as far as known (None: all of k), lse: float32 (heads_q, rows_q) or None, workspace: uint8 of
+    lop_attention_workspace bytes (None: allocated). Returns out."""
+    dtype = _dtype("q", q)
+    i32 = torch.int32
+    stream = _tensors(("q", q, 3, q.dtype), ("k", k, 3, q.dtype), ("v", v, 3, q.dtype), ("q_offsets", q_offsets, 1, i32),
+                      ("k_begin", k_begin, 1, i32), ("k_end", k_end, 1, i32), ("out", out, 3, q.dtype), ("lse", lse, 2, torch.float32),
+                      ("workspace", workspace, 1, torch.uint8))
+    rows_q, hq, d = q.shape
+    rows_k, hk, _ = k.shape
+    seqs = k_begin.shape[0]
+    if out is None:
+        out = torch.empty((rows_q, hq, d), dtype=q.dtype, device=q.device)
+    _need(k.shape[2] == d and v.shape == k.shape and out.shape == q.shape, "head sizes, or shapes of k and v or q and out, differ")
+    _need(q_offsets.shape == (seqs + 1,) and k_end.shape == (seqs,), "q_offsets has an entry more than k_begin and k_end")
+    _need(lse is None or (lse.shape == (hq, rows_q) and lse.is_contiguous()), f"lse is {(hq, rows_q)}, dense")
+    for name, t in (("q", q), ("k", k), ("v", v), ("out", out), ("q_offsets", q_offsets), ("k_begin", k_begin), ("k_end", k_end),
+                    ("workspace", workspace)):
+        _inner(name, t)
+    qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), out.stride()   # (of no row: not looked at)
+    op = lop_attention_t(dtype, hq, hk, d, seqs, rows_q, rows_k, rows_k if max_keys is None else max_keys, int(causal), scale,
+                         q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
+                         out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), _at(lse), None, 0)
+    band = _band(rows, rows_q)
+    if workspace is None:
+        n = c_ulonglong(0)
+        _check(_lib.lop_attention_workspace(byref(op), band, byref(n)), "lop_attention_workspace")
+        if n.value:
+            workspace = torch.empty(n.value, dtype=torch.uint8, device=q.device)
+    if workspace is not None:
+        op.workspace, op.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(_lib.lop_attention(byref(op), band, stream), "lop_attention")
+    return out
