@@ -419,7 +419,7 @@ Cut cut(const lop_attention_t* op, lop_rows_t rows) {
   c.tiles = (int)((rows.hi * group - 1) / kRows + op->seqs - c.tile0);
   // Two workgroups fit a compute unit. Where there are fewer than that the keys are cut into parts of 256 at least.
   const long long blocks = (long long)c.tiles * op->heads_k;
-  c.splits = (int)std::max(1LL, std::min({ceil_div(1024, blocks), (long long)std::max(op->max_keys, 1) / 256, 64LL}));
+  c.splits = (int)std::max(1LL, std::min({ceil_div(1024, blocks), (long long)op->max_keys / (LOP_ATTENTION_CUT / 2), 64LL}));
   if (blocks >= 512) c.splits = 1;
   return c;
 }

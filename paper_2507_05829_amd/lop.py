@@ -39,7 +39,7 @@ LOP_FLAG_NO_FUSE = 32
 LOP_FLAG_POISON_SCRATCH = 64
 LOP_FLAG_BATCH_BANDS = 128
 LOP_LINK_INDEPENDENT, LOP_LINK_QUEUED = 0, 1
-LOP_F8_BLOCK = 128
+LOP_F8_BLOCK, LOP_ATTENTION_CUT = 128, 512
 
 
 def LOP_FLAG_LANES(n: int) -> int:
@@ -590,66 +590,79 @@ _TYPES = {getattr(torch, n): c for n, c in (("float32", LOP_F32), ("bfloat16", L
 _F8 = getattr(torch, "float8_e4m3fn", None)
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+def _bad(name: str, what: str):
+    raise ValueError(f"{name}: {what}")
 
 
-def _tensors(*named) -> int:
-    """Checks that (name, tensor, dimensions, type) are tensors of the current device; None is passed over. Returns the
-    current stream."""
-    device = torch.cuda.current_device()
-    grad = torch.is_grad_enabled()
-    for name, t, dims, dtype in named:
-        if t is None:
-            continue
-        if t.dim() != dims or t.dtype != dtype:
-            raise ValueError(f"{name}: {dims} dimensions of {dtype} are wanted, not {t.dim()} of {t.dtype}")
-        if not t.is_cuda or t.get_device() != device:
-            raise ValueError(f"{name}: on {t.device}, not on the current device ({device})")
-        if grad and t.requires_grad:
-            raise ValueError(f"{name}: forward only, but the tensor wants a gradient")
-    return torch._C._cuda_getCurrentRawStream(device)
+def _fits(name: str, t, dtype, device: int, grad: bool) -> None:
+    """The tensor is of this type, on this device, its values next to one another and no gradient is wanted of it."""
+    if t.dtype is not dtype:
+        _bad(name, f"{dtype} is wanted, not {t.dtype}")
+    if t.get_device() != device:
+        _bad(name, f"on {t.device}, not on the current device ({device})")
+    if grad and t.requires_grad:
+        _bad(name, "forward only, but the tensor wants a gradient")
+
+
+def _rows_of(name: str, t, dtype, device: int, grad: bool):
+    """The strides of a tensor that _fits, its values next to one another in a row."""
+    if t.dtype is not dtype or t.get_device() != device or (grad and t.requires_grad):
+        _fits(name, t, dtype, device, grad)
+    strides = t.stride()
+    if strides[-1] != 1 and t.shape[-1] > 1 and t.numel() > 0:
+        _bad(name, "the values of a row have to lie next to one another")
+    return strides
+
+
+def _shaped(name: str, t, shape) -> None:
+    if t.shape != shape:
+        _bad(name, f"{tuple(shape)} is wanted, not {tuple(t.shape)}")
+
+
+def _dims(name: str, t, n: int):
+    if t.dim() != n:
+        _bad(name, f"{n} dimensions are wanted, not {t.dim()}")
+    return t.shape
 
 
 def _dtype(name: str, t: torch.Tensor) -> int:
     code = _TYPES.get(t.dtype)
     if code is None:
-        raise ValueError(f"{name}: float32 or bfloat16 is wanted, not {t.dtype}")
+        _bad(name, f"float32 or bfloat16 is wanted, not {t.dtype}")
     return code
-
-
-def _inner(name: str, t) -> None:
-    if t is not None and t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel() > 0:
-        raise ValueError(f"{name}: the values of a row have to lie next to one another")
-
-
-def _at(t):
-    return None if t is None else t.data_ptr()
 
 
 def _band(rows, total: int) -> lop_rows_t:
     return lop_rows_t(0, total) if rows is None else lop_rows_t(*rows)
 
 
+def _here():
+    """The current device, its current stream, whether gradients are recorded."""
+    device = torch.cuda.current_device()
+    return device, torch._C._cuda_getCurrentRawStream(device), torch.is_grad_enabled()
+
+
 def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
     """x (m, k) in e4m3 with a scale for each block of `block_rows` x 128 values (see lop_quantize_blocks). Returns
     (q, scale): q float8_e4m3fn (m, k), scale float32 (ceil(m / block_rows), ceil(k / 128)), allocated with the scales
     of a column of blocks next to one another."""
+    device, stream, grad = _here()
     dtype = _dtype("x", x)
-    stream = _tensors(("x", x, 2, x.dtype), ("q", q, 2, _F8), ("scale", scale, 2, torch.float32))
-    m, k = x.shape
-    _need(block_rows in (1, LOP_F8_BLOCK), f"block_rows: 1 or {LOP_F8_BLOCK}")
+    m, k = _dims("x", x, 2)
+    if block_rows != 1 and block_rows != LOP_F8_BLOCK:
+        _bad("block_rows", f"1 or {LOP_F8_BLOCK}")
     shape = (-(-m // block_rows), -(-k // LOP_F8_BLOCK))
     if q is None:
         q = torch.empty((m, k), dtype=_F8, device=x.device)
     if scale is None:
         scale = torch.empty(shape[::-1], dtype=torch.float32, device=x.device).t()
-    _need(q.shape == x.shape and scale.shape == shape, f"q is {tuple(x.shape)} and scale {shape}")
-    _inner("x", x)
-    _inner("q", q)
-    op = lop_quantize_t(m, k, dtype, block_rows, x.data_ptr(), x.stride(0), q.data_ptr(), q.stride(0), scale.data_ptr(),
-                        scale.stride(0), scale.stride(1))
+    xs = _rows_of("x", x, x.dtype, device, grad)
+    qs = _rows_of("q", q, _F8, device, grad)
+    _fits("scale", scale, torch.float32, device, grad)
+    _shaped("q", q, x.shape)
+    _shaped("scale", scale, shape)
+    s0, s1 = scale.stride()
+    op = lop_quantize_t(m, k, dtype, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), s0, s1)
     _check(_lib.lop_quantize_blocks(byref(op), _band(rows, m), stream), "lop_quantize_blocks")
     return q, scale
 
@@ -657,25 +670,39 @@ def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
 def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=None, y=None, dtype=None, rows=None):
     """act(x W^T + bias + residual) of operands quantized by quantize_blocks: x (m, k) with blocks of one row, w (n, k)
     with blocks of 128 rows (see lop_rowwise_f8). y (m, n) is allocated in `dtype` (None: bfloat16) if it is not passed."""
-    dtype = y.dtype if y is not None else dtype or torch.bfloat16
-    _need(dtype in _TYPES, "y: float32 or bfloat16")
-    _need(act in _ACTS, f"act: one of {sorted(_ACTS)}")
-    f32 = torch.float32
-    stream = _tensors(("x", x, 2, _F8), ("x_scale", x_scale, 2, f32), ("w", w, 2, _F8), ("w_scale", w_scale, 2, f32),
-                      ("bias", bias, 1, f32), ("residual", residual, 2, dtype), ("y", y, 2, dtype))
-    m, k = x.shape
-    n, kb = w.shape[0], -(-k // LOP_F8_BLOCK)
+    device, stream, grad = _here()
+    m, k = _dims("x", x, 2)
+    n, kw = _dims("w", w, 2)
+    kb = -(-k // LOP_F8_BLOCK)
+    if act not in _ACTS:
+        _bad("act", f"one of {sorted(_ACTS)}")
     if y is None:
-        y = torch.empty((m, n), dtype=dtype, device=x.device)
-    _need(w.shape[1] == k, "x and w have different numbers of columns")
-    _need(x_scale.shape == (m, kb) and w_scale.shape == (-(-n // LOP_F8_BLOCK), kb), "scales do not fit their matrices")
-    _need(y.shape == (m, n) and (residual is None or residual.shape == (m, n)) and (bias is None or bias.shape == (n,)),
-          f"y and residual are {(m, n)}, bias {(n,)}")
-    for name, t in (("x", x), ("w", w), ("bias", bias), ("residual", residual), ("y", y)):
-        _inner(name, t)
-    op = lop_rowwise_f8_t(m, n, k, _TYPES[dtype], _ACTS[act], x.data_ptr(), x.stride(0), x_scale.data_ptr(), x_scale.stride(0),
-                          x_scale.stride(1), w.data_ptr(), w.stride(0), w_scale.data_ptr(), w_scale.stride(0), w_scale.stride(1),
-                          _at(bias), _at(residual), 0 if residual is None else residual.stride(0), y.data_ptr(), y.stride(0))
+        y = torch.empty((m, n), dtype=dtype or torch.bfloat16, device=x.device)
+    code, dtype, f32 = _dtype("y", y), y.dtype, torch.float32
+    if kw != k:
+        _bad("w", f"{k} columns are wanted, not {kw}")
+    xs = _rows_of("x", x, _F8, device, grad)
+    ws = _rows_of("w", w, _F8, device, grad)
+    _fits("x_scale", x_scale, f32, device, grad)
+    _fits("w_scale", w_scale, f32, device, grad)
+    ys = _rows_of("y", y, dtype, device, grad)
+    _shaped("x_scale", x_scale, (m, kb))
+    _shaped("w_scale", w_scale, (-(-n // LOP_F8_BLOCK), kb))
+    _shaped("y", y, (m, n))
+    bias_at = residual_at = None
+    residual_stride = 0
+    if bias is not None:
+        _rows_of("bias", bias, f32, device, grad)
+        _shaped("bias", bias, (n,))
+        bias_at = bias.data_ptr()
+    if residual is not None:
+        residual_stride = _rows_of("residual", residual, dtype, device, grad)[0]
+        _shaped("residual", residual, (m, n))
+        residual_at = residual.data_ptr()
+    xs0, xs1 = x_scale.stride()
+    ws0, ws1 = w_scale.stride()
+    op = lop_rowwise_f8_t(m, n, k, code, _ACTS[act], x.data_ptr(), xs[0], x_scale.data_ptr(), xs0, xs1, w.data_ptr(), ws[0],
+                          w_scale.data_ptr(), ws0, ws1, bias_at, residual_at, residual_stride, y.data_ptr(), ys[0])
     _check(_lib.lop_rowwise_f8(byref(op), _band(rows, m), stream), "lop_rowwise_f8")
     return y
 
@@ -685,31 +712,42 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
     """q (tokens, heads_q, d) and k (tokens, heads_k, d) or None, each head normalized (where its weight (d,) is given) and its first
     2 * len(freq) values rotated by positions * freq (see lop_head_norm_rope). positions int32 (tokens,), freq float32,
     both None for no rotation. Returns (q_out, k_out), which may be q and k."""
-    dtype = _dtype("q", q)
-    f32 = torch.float32
-    stream = _tensors(("q", q, 3, q.dtype), ("k", k, 3, q.dtype), ("positions", positions, 1, torch.int32), ("freq", freq, 1, f32),
-                      ("q_weight", q_weight, 1, f32), ("k_weight", k_weight, 1, f32), ("q_out", q_out, 3, q.dtype),
-                      ("k_out", k_out, 3, q.dtype))
-    tokens, hq, d = q.shape
-    hk = 0 if k is None else k.shape[1]
+    device, stream, grad = _here()
+    code, dtype, f32 = _dtype("q", q), q.dtype, torch.float32
+    tokens, hq, d = _dims("q", q, 3)
     if q_out is None:
-        q_out = torch.empty((tokens, hq, d), dtype=q.dtype, device=q.device)
-    if k_out is None and k is not None:
-        k_out = torch.empty((tokens, hk, d), dtype=q.dtype, device=q.device)
-    _need(k is None or k.shape == (tokens, hk, d), "q and k have different tokens or head sizes")
-    _need(q_out.shape == q.shape and (k is None or k_out.shape == k.shape), "outputs have their inputs' shapes")
-    _need((positions is None) == (freq is None), "positions and freq go together")
-    _need(positions is None or positions.shape == (tokens,), "a position for each token")
-    for name, t in (("q_weight", q_weight), ("k_weight", k_weight)):
-        _need(t is None or t.shape == (d,), f"{name}: a value for each of a head's")
-    for name, t in (("q", q), ("k", k), ("positions", positions), ("freq", freq), ("q_weight", q_weight), ("k_weight", k_weight),
-                    ("q_out", q_out), ("k_out", k_out)):
-        _inner(name, t)
-    ks, kos = (0, 0, 0) if k is None else k.stride(), (0, 0, 0) if k is None else k_out.stride()
-    qs, qos = q.stride(), q_out.stride()
-    op = lop_head_norm_rope_t(tokens, hq, hk, d, 0 if freq is None else 2 * freq.shape[0], int(interleaved), dtype, eps, amplitude,
-                              q.data_ptr(), qs[0], qs[1], _at(k), ks[0], ks[1], q_out.data_ptr(), qos[0], qos[1],
-                              _at(k_out), kos[0], kos[1], _at(q_weight), _at(k_weight), _at(positions), _at(freq))
+        q_out = torch.empty((tokens, hq, d), dtype=dtype, device=q.device)
+    qs = _rows_of("q", q, dtype, device, grad)
+    qos = _rows_of("q_out", q_out, dtype, device, grad)
+    _shaped("q_out", q_out, q.shape)
+    hk, k_at, k_out_at, ks, kos = 0, None, None, (0, 0), (0, 0)
+    if k is not None:
+        hk = _dims("k", k, 3)[1]
+        if k_out is None:
+            k_out = torch.empty((tokens, hk, d), dtype=dtype, device=q.device)
+        ks = _rows_of("k", k, dtype, device, grad)
+        kos = _rows_of("k_out", k_out, dtype, device, grad)
+        _shaped("k", k, (tokens, hk, d))
+        _shaped("k_out", k_out, k.shape)
+        k_at, k_out_at = k.data_ptr(), k_out.data_ptr()
+    if (positions is None) != (freq is None):
+        _bad("positions", "they and freq go together")
+    turns, positions_at, freq_at = 0, None, None
+    if freq is not None:
+        _rows_of("positions", positions, torch.int32, device, grad)
+        _rows_of("freq", freq, f32, device, grad)
+        turns = _dims("freq", freq, 1)[0]
+        _shaped("positions", positions, (tokens,))
+        positions_at, freq_at = positions.data_ptr(), freq.data_ptr()
+    weights = [None, None]
+    for i, t in enumerate((q_weight, k_weight)):
+        if t is not None:
+            _rows_of("weight", t, f32, device, grad)
+            _shaped("weight", t, (d,))
+            weights[i] = t.data_ptr()
+    op = lop_head_norm_rope_t(tokens, hq, hk, d, 2 * turns, interleaved, code, eps, amplitude, q.data_ptr(), qs[0], qs[1],
+                              k_at, ks[0], ks[1], q_out.data_ptr(), qos[0], qos[1], k_out_at, kos[0], kos[1],
+                              weights[0], weights[1], positions_at, freq_at)
     _check(_lib.lop_head_norm_rope(byref(op), _band(rows, tokens), stream), "lop_head_norm_rope")
     return q_out, k_out
 
@@ -720,33 +758,47 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
     i's queries are rows q_offsets[i] .. q_offsets[i + 1], its keys rows k_begin[i] .. k_end[i] (int32 tensors). max_keys: keys of the longest
     sequence as far as known (None: all of k), lse: float32 (heads_q, rows_q) or None, workspace: uint8 of
     lop_attention_workspace bytes (None: allocated). Returns out."""
-    dtype = _dtype("q", q)
-    i32 = torch.int32
-    stream = _tensors(("q", q, 3, q.dtype), ("k", k, 3, q.dtype), ("v", v, 3, q.dtype), ("q_offsets", q_offsets, 1, i32),
-                      ("k_begin", k_begin, 1, i32), ("k_end", k_end, 1, i32), ("out", out, 3, q.dtype), ("lse", lse, 2, torch.float32),
-                      ("workspace", workspace, 1, torch.uint8))
-    rows_q, hq, d = q.shape
-    rows_k, hk, _ = k.shape
-    seqs = k_begin.shape[0]
+    device, stream, grad = _here()
+    code, dtype, i32 = _dtype("q", q), q.dtype, torch.int32
+    rows_q, hq, d = _dims("q", q, 3)
+    rows_k, hk, _ = _dims("k", k, 3)
+    seqs = _dims("k_begin", k_begin, 1)[0]
     if out is None:
-        out = torch.empty((rows_q, hq, d), dtype=q.dtype, device=q.device)
-    _need(k.shape[2] == d and v.shape == k.shape and out.shape == q.shape, "head sizes, or shapes of k and v or q and out, differ")
-    _need(q_offsets.shape == (seqs + 1,) and k_end.shape == (seqs,), "q_offsets has an entry more than k_begin and k_end")
-    _need(lse is None or (lse.shape == (hq, rows_q) and lse.is_contiguous()), f"lse is {(hq, rows_q)}, dense")
-    for name, t in (("q", q), ("k", k), ("v", v), ("out", out), ("q_offsets", q_offsets), ("k_begin", k_begin), ("k_end", k_end),
-                    ("workspace", workspace)):
-        _inner(name, t)
-    qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), out.stride()   # (of no row: not looked at)
-    op = lop_attention_t(dtype, hq, hk, d, seqs, rows_q, rows_k, rows_k if max_keys is None else max_keys, int(causal), scale,
+        out = torch.empty((rows_q, hq, d), dtype=dtype, device=q.device)
+    qs = _rows_of("q", q, dtype, device, grad)
+    ks = _rows_of("k", k, dtype, device, grad)
+    vs = _rows_of("v", v, dtype, device, grad)
+    os_ = _rows_of("out", out, dtype, device, grad)
+    _rows_of("q_offsets", q_offsets, i32, device, grad)
+    _rows_of("k_begin", k_begin, i32, device, grad)
+    _rows_of("k_end", k_end, i32, device, grad)
+    _shaped("k", k, (rows_k, hk, d))
+    _shaped("v", v, k.shape)
+    _shaped("out", out, q.shape)
+    _shaped("q_offsets", q_offsets, (seqs + 1,))
+    _shaped("k_end", k_end, (seqs,))
+    lse_at = None
+    if lse is not None:
+        _fits("lse", lse, torch.float32, device, grad)
+        _shaped("lse", lse, (hq, rows_q))
+        if not lse.is_contiguous():
+            _bad("lse", "dense rows are wanted")
+        lse_at = lse.data_ptr()
+    if max_keys is None:
+        max_keys = rows_k
+    op = lop_attention_t(code, hq, hk, d, seqs, rows_q, rows_k, max_keys, causal, scale,
                          q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
-                         out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), _at(lse), None, 0)
+                         out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), lse_at, None, 0)
     band = _band(rows, rows_q)
-    if workspace is None:
+    if workspace is None and max_keys >= LOP_ATTENTION_CUT:
         n = c_ulonglong(0)
         _check(_lib.lop_attention_workspace(byref(op), band, byref(n)), "lop_attention_workspace")
         if n.value:
             workspace = torch.empty(n.value, dtype=torch.uint8, device=q.device)
     if workspace is not None:
+        _fits("workspace", workspace, torch.uint8, device, grad)
+        if not workspace.is_contiguous():
+            _bad("workspace", "dense memory is wanted")
         op.workspace, op.workspace_bytes = workspace.data_ptr(), workspace.numel()
     _check(_lib.lop_attention(byref(op), band, stream), "lop_attention")
     return out
