@@ -29,6 +29,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr unsigned kOut = 0x80000000u;
 constexpr int kRows = 128;            // of a workgroup: 32 for each of four wavefronts
+constexpr float kSlack = 8.f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 struct AttnParams {
@@ -75,6 +76,21 @@ __device__ __forceinline__ float sum_of_halves(float v) {
   return __uint_as_float((unsigned)s[0]) + __uint_as_float((unsigned)s[1]);
 }
 
+// a product with the sum of products before it, which is none
+template <typename T>
+__device__ __forceinline__ f32x16 mma_first(const u32x4& a, const u32x4& b) {
+  const f32x16 none = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), none, 0, 0, 0);
+  } else {
+    const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+    f32x16 s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[0], y[0], none, 0, 0, 0);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], s, 0, 0, 0);
+    return s;
+  }
+}
+
 constexpr int attn_pitch(int bytes) { return bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
 
 // DP: head_dim rounded up to what is computed (a multiple of 32)
@@ -83,7 +99,7 @@ struct AttnShape {
   static constexpr int E = (int)sizeof(T);
   static constexpr int PITCH = attn_pitch(DP * E);       // bytes of a key in LDS
   static constexpr int CP = PITCH / 16;                  // 16-byte chunks of it
-  static constexpr int KT = PITCH <= 512 ? 64 : 32;      // keys of a tile
+  static constexpr int KT = E == 4 && PITCH >= 512 ? 32 : 64;   // keys of a tile (two workgroups' tiles fit a compute unit up to 128 values)
   static constexpr int BYTES = KT * PITCH;
   static constexpr int LDS = 4 * BYTES;                  // two tiles of keys and of values
   static constexpr int LD = BYTES / 4096;                // load instructions of a wavefront for one tile of either
@@ -197,10 +213,8 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 
   const float c = p.scale * kLog2e;
   f32x16 o[DT];
-  float m, l;   // maximum of c s, in powers of two; sum
-  // Weights of zero times an infinity or a NaN of a value that the row does not see are NaNs. They are rare, and looked for at the end only: then the
-  // keys are gone through again, those of tiles that some row sees in part one by one.
-  for (int careful = 0; careful < 2; ++careful) {
+  float m, l;   // what the exponents of c s are relative to, in powers of two; sum
+  auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -213,26 +227,51 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
       barrier();
       if (t + 1 < t1) issue(t + 1, (t + 1 - t0) & 1);
       if (t * KT >= most) continue;
-      const unsigned buf = (unsigned)(((t - t0) & 1) * 2 * S::BYTES);
-      // scores
-      f32x16 s[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-        constexpr int G = KS % 8 == 0 ? 8 : KS;   // reads in flight
-#pragma unroll
-        for (int k0 = 0; k0 < KS; k0 += G) {
-          u32x4 fk[G];
-#pragma unroll
-          for (int i = 0; i < G; ++i)
-            asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(fk[i]) : "v"((k_at + buf) ^ (unsigned)((k0 + i) * 32)), "n"(b * 32 * PITCH) : "memory");
-          unroll<G>([&](auto i) __attribute__((always_inline)) {
-            asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(fk[i]) : "n"(G - 1 - i) : "memory");
-            mma<T>(fk[i], fq[k0 + i], s[b]);
-          });
+      const unsigned buf = (unsigned)(((t - t0) & 1) * 2 * S::BYTES), kb = k_at + buf, vb = v_at + buf;
+
+      // The values' operands come in chunks: of 16 keys (fp32: two) and up to 128 columns, two reads (one) for each 32 columns. A chunk is read while the one
+      // before it is multiplied, the first one behind the keys.
+      constexpr int G = E == 4 ? DT : DT % 4 == 0 ? 4 : DT, PER = E == 4 ? 1 : 2, CHUNK = G * PER, CHUNKS = (E == 4 ? NB * 16 : NB * 2) * (DT / G);
+      u32x2 fv[2][CHUNK];   // (fp32: the first of two)
+      auto read_v = [&](auto chunk, auto r) __attribute__((always_inline)) {   // read r of a chunk
+        u32x2& to = fv[chunk & 1][r];
+        constexpr int step = chunk / (DT / G), d = chunk % (DT / G) * G + r / PER;
+        if constexpr (E == 2) {
+          const unsigned at = vb ^ (unsigned)(d * 64);
+          // Of 16 lanes, lane i gets value i % 4 of the four that lanes i / 4, i / 4 + 4, + 8 and + 12 point at: four keys of one of 16 columns.
+          asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(to) : "v"(at), "n"((step * 16 + r % 2 * 8) * PITCH) : "memory");
+        } else {
+          const unsigned at = vb ^ (unsigned)(d * 128);
+          float got;
+          asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(got) : "v"(at), "n"((step / 16 * 32 + step % 16 / 4 * 8 + step % 4) * PITCH) : "memory");
+          to[0] = __float_as_uint(got);
         }
-      }
+      };
+
+      // scores: steps of 16 bytes of 32 keys, RING reads ahead; the two blocks of keys in turn, so that no product waits for the one before it
+      constexpr int STEPS = KS * NB, RING = STEPS < 8 ? STEPS : 8;
+      f32x16 s[NB];
+      u32x4 fk[RING];
+      auto read_k = [&](auto step) __attribute__((always_inline)) {
+        u32x4& to = fk[step % RING];
+        const unsigned at = kb ^ (unsigned)(step / NB * 32);
+        asm volatile("ds_read_b128 %0, %1 offset:%2" : "=v"(to) : "v"(at), "n"(step % NB * 32 * PITCH) : "memory");
+      };
+      unroll<RING>([&](auto i) __attribute__((always_inline)) { read_k(i); });
+      unroll<STEPS>([&](auto i) __attribute__((always_inline)) {
+        constexpr int behind = i - (STEPS - RING);   // steps without a read of keys so far
+        constexpr int younger = (i + RING <= STEPS ? RING - 1 : STEPS - 1 - i) + (careful || behind < 0 ? 0 : behind < CHUNK ? behind : CHUNK);
+        u32x4& f = fk[i % RING];
+        asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(f) : "n"(younger) : "memory");
+        if constexpr (i < NB) s[i] = mma_first<T>(f, fq[0]);
+        else mma<T>(f, fq[i / NB], s[i % NB]);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (i + RING < STEPS) read_k(std::integral_constant<int, i + RING>{});
+        else if constexpr (!careful && behind < CHUNK) read_v(std::integral_constant<int, 0>{}, std::integral_constant<int, behind>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+      if constexpr (!careful) unroll<(CHUNK > RING ? CHUNK - RING : 0)>([&](auto r) __attribute__((always_inline)) { read_v(std::integral_constant<int, 0>{}, std::integral_constant<int, RING + r>{}); });
+
       const bool partly = t * KT + KT > least;
       if (partly) {
         const int upto = sees - t * KT - 4 * half;
@@ -241,15 +280,20 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[b][i] = b * 32 + (i / 4) * 8 + i % 4 < upto ? s[b][i] : -INFINITY;
       }
-      // maximum
-      float top = s[0][0];
+      // What the exponents are relative to need not be the maximum: it follows where that has grown by more than 2^kSlack, so that sums and
+      // output are hardly ever multiplied.
+      float top[NB];
 #pragma unroll
-      for (int b = 0; b < NB; ++b)
+      for (int b = 0; b < NB; ++b) {
+        top[b] = s[b][0];
 #pragma unroll
-        for (int i = b ? 0 : 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[b][i]);
-      const float grown = __builtin_elementwise_maximum(m, max_of_halves(top) * c);
-      if (__any(grown != m)) {
-        const float by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
+        for (int i = 1; i < 16; ++i) top[b] = __builtin_elementwise_maximum(top[b], s[b][i]);
+      }
+#pragma unroll
+      for (int b = 1; b < NB; ++b) top[0] = __builtin_elementwise_maximum(top[0], top[b]);
+      const float now = max_of_halves(top[0]) * c;
+      if (__any(!(now <= m + kSlack))) {
+        const float grown = __builtin_elementwise_maximum(m, now), by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
         m = grown;
         l *= by;
 #pragma unroll
@@ -258,15 +302,17 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
           for (int i = 0; i < 16; ++i) o[d][i] *= by;
       }
       const float from = m == -INFINITY ? 0.f : m;   // (no key so far)
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -from));
-          l += s[b][i];
+          part[i & 3] += s[b][i];
         }
+      l += (part[0] + part[1]) + (part[2] + part[3]);
       // output
-      if (careful && partly) {
+      if constexpr (careful) {
         const int upto = sees - t * KT;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -292,58 +338,45 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
                 }
             }
           }
-        continue;
-      }
-      if constexpr (E == 2) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {   // 16 keys: the operand's eight of a lane are keys 4 half + {0..3} and 8 on of them
+      } else {
+        u32x4 fw;
+        unroll<CHUNKS>([&](auto chunk) __attribute__((always_inline)) {
+          constexpr bool last = chunk == CHUNKS - 1;
+          constexpr int step = chunk / (DT / G), d0 = chunk % (DT / G) * G;
+          if constexpr (!last) unroll<CHUNK>([&](auto r) __attribute__((always_inline)) { read_v(std::integral_constant<int, chunk + 1>{}, r); });
+          if constexpr (E == 2 && d0 == 0) {   // 16 keys: the operand's eight of a lane are keys 4 half + {0..3} and 8 on of them
             alignas(16) __bf16 w[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = (__bf16)s[b][h * 8 + i];
-            const u32x4 fw = *(const u32x4*)w;
-            // Of 16 lanes, lane i gets value i % 4 of the four that lanes i / 4, i / 4 + 4, + 8 and + 12 point at: four keys of one of 16 columns.
-            constexpr int G = DT < 4 ? DT : 4;
-#pragma unroll
-            for (int d0 = 0; d0 < DT; d0 += G) {
-              u32x2 fv[G][2];
-#pragma unroll
-              for (int d = 0; d < G; ++d) {
-                const unsigned at = (v_at + buf) ^ (unsigned)((d0 + d) * 64);
-                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(fv[d][0]) : "v"(at), "n"((b * 32 + h * 16) * PITCH) : "memory");
-                asm volatile("ds_read_b64_tr_b16 %0, %1 offset:%2" : "=v"(fv[d][1]) : "v"(at), "n"((b * 32 + h * 16 + 8) * PITCH) : "memory");
-              }
-              unroll<G>([&](auto d) __attribute__((always_inline)) {
-                asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(fv[d][0]), "+v"(fv[d][1]) : "n"(2 * (G - 1 - d)) : "memory");
-                mma<T>(u32x4{fv[d][0][0], fv[d][0][1], fv[d][1][0], fv[d][1][1]}, fw, o[d0 + d]);
-              });
+            for (int i = 0; i < 8; ++i) w[i] = (__bf16)s[step / 2][step % 2 * 8 + i];
+            fw = *(const u32x4*)w;
+          }
+          __builtin_amdgcn_sched_barrier(0);
+          unroll<G>([&](auto d) __attribute__((always_inline)) {
+            constexpr int younger = PER * (G - 1 - d) + (last ? 0 : CHUNK);
+            if constexpr (E == 2) {
+              u32x2 &a = fv[chunk & 1][2 * d], &b = fv[chunk & 1][2 * d + 1];
+              asm volatile("s_waitcnt lgkmcnt(%2)" : "+v"(a), "+v"(b) : "n"(younger) : "memory");
+              mma<T>(u32x4{a[0], a[1], b[0], b[1]}, fw, o[d0 + d]);
+            } else {
+              float a = __uint_as_float(fv[chunk & 1][d][0]);
+              asm volatile("s_waitcnt lgkmcnt(%1)" : "+v"(a) : "n"(younger) : "memory");
+              o[d0 + d] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, s[step / 16][step % 16], o[d0 + d], 0, 0, 0);
             }
-          }
-      } else {
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {   // two keys: one of either half
-            float fv[DT];
-#pragma unroll
-            for (int d = 0; d < DT; ++d)
-              asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(fv[d]) : "v"((v_at + buf) ^ (unsigned)(d * 128)), "n"((b * 32 + (i / 4) * 8 + i % 4) * PITCH) : "memory");
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll
-            for (int d = 0; d < DT; ++d) asm volatile("" : "+v"(fv[d]));
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(fv[d], s[b][i], o[d], 0, 0, 0);
-          }
+          });
+          __builtin_amdgcn_sched_barrier(0);
+        });
       }
     }
-    bool odd = false;
+  };
+  pass(std::false_type{});
+  // Weights of zero times an infinity or a NaN of a value that the row does not see are NaNs. They are rare, and looked for at the end only: then the
+  // keys are gone through again, one by one.
+  bool odd = false;
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) odd |= live && !(fabsf(o[d][i]) < INFINITY);
-    if (careful || !__syncthreads_or(odd)) break;
-  }
+    for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) < INFINITY);
+  if (__syncthreads_or(odd && live)) pass(std::true_type{});
   l = sum_of_halves(l);
   if (!live) return;
 
