@@ -10,7 +10,7 @@
 // mirror image 32 lanes on: a maximum over keys is one over registers and one exchange, and the weights lie as the product with the values
 // (v^T w^T) wants its second operand, whose order of keys is free as long as both operands have the same. Four
 // wavefronts share tiles of KT keys and values, which travel from memory to LDS without passing through registers, one
-// tile ahead.
+// tile ahead. Where there are few workgroups the keys are cut into parts, and a second kernel joins their results.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -38,7 +38,7 @@ struct AttnParams {
   long long q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;   // bytes
   const int *q_offsets, *k_begin, *k_end;
   float* lse;
-  float* part;       // [split][row of q][head][head_dim + 2]: output so far, maximum, sum
+  float* part;       // of keys cut into parts: [split][row of the band][head][head_dim] of the output, then [..][2] of maximum and sum
   int heads_k, group, head_dim, seqs, rows_q, rows_k, causal;
   int lo, hi;        // the band
   int tile0, tiles;  // of packed rows
@@ -381,16 +381,17 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
   if (!live) return;
 
   if (p.splits > 1) {
-    const long long slot = ((long long)blockIdx.y * (p.hi - p.lo) + at_row - p.lo) * (p.heads_k * p.group) + qh;
-    float* const to = p.part + slot * (p.head_dim + 2);
+    const long long rows = (long long)(p.hi - p.lo) * (p.heads_k * p.group);
+    const long long slot = blockIdx.y * rows + (at_row - p.lo) * (p.heads_k * p.group) + qh;
+    float* const to = p.part + slot * p.head_dim;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int at = d * 32 + (i / 4) * 8 + half * 4 + i % 4;
-        if (at < p.head_dim) to[at] = o[d][i];
+      for (int j = 0; j < 4; ++j) {
+        const int at = d * 32 + j * 8 + half * 4;
+        if (at < p.head_dim) *(f32x4*)(to + at) = f32x4{o[d][j * 4], o[d][j * 4 + 1], o[d][j * 4 + 2], o[d][j * 4 + 3]};
       }
-    if (half == 0) { to[p.head_dim] = m; to[p.head_dim + 1] = sees > 0 ? l : -1.f; }
+    if (half == 0) *(float2*)(p.part + p.splits * rows * p.head_dim + slot * 2) = make_float2(m, sees > 0 ? l : -1.f);
     return;
   }
   const float by = sees > 0 ? 1.f / l : 0.f;
@@ -409,31 +410,37 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
   if (p.lse && half == 0) p.lse[(long long)qh * p.rows_q + at_row] = sees > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
-// Joins the parts of a row: a wavefront for each row and head. (A sum of -1: the row sees no key.)
+// Joins the parts of a row: a wavefront for each row and head, lane s has part s's maximum and sum. (A sum of -1: the row sees no key.)
 template <typename T>
 __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p) {
   const int lane = threadIdx.x & 63, heads = p.heads_k * p.group;
-  const long long at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long long rows = (long long)(p.hi - p.lo) * heads, at = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (at >= rows) return;
   const int head = (int)(at % heads);
   const long long row = p.lo + at / heads;
   const int first = clamp_to(p.q_offsets[0], p.rows_q), last = clamp_to(p.q_offsets[p.seqs], p.rows_q);
-  if (row >= p.hi || row < first || row >= last) return;
-  const long long pitch = p.head_dim + 2, step = (long long)(p.hi - p.lo) * heads * pitch;
-  const float* const parts = p.part + at * pitch;
-  float m = -INFINITY;
-  for (int s = 0; s < p.splits; ++s) m = __builtin_elementwise_maximum(m, parts[s * step + p.head_dim]);
-  const float from = m == -INFINITY ? 0.f : m;
-  float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-  const bool here = lane * 4 < p.head_dim;
-  for (int s = 0; s < p.splits; ++s) {
-    const float* const x = parts + s * step;
-    const float by = __builtin_amdgcn_exp2f(x[p.head_dim] - from);
-    l = fmaf(by, x[p.head_dim + 1], l);
-    if (here)
+  if (row < first || row >= last) return;
+  const float2* const stats = (const float2*)(p.part + p.splits * rows * p.head_dim);
+  const float2 mine = lane < p.splits ? stats[lane * rows + at] : make_float2(-INFINITY, 0.f);
+  float m = mine.x;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = fmaf(by, x[lane * 4 + i], o[i]);
+  for (int d = 1; d < 64; d *= 2) m = __builtin_elementwise_maximum(m, __shfl_xor(m, d, 64));
+  const float by = __builtin_amdgcn_exp2f(mine.x - (m == -INFINITY ? 0.f : m));
+  const bool none = __any(mine.y < 0.f);
+  float l = by * mine.y;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d, 64);
+  const bool here = lane * 4 < p.head_dim;
+  const float* const from = p.part + at * p.head_dim + (here ? lane * 4 : 0);
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int s0 = 0; s0 < p.splits; s0 += 8) {   // (the last part again where there are fewer, and nothing of it)
+    f32x4 x[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = *(const f32x4*)(from + min(s0 + i, p.splits - 1) * rows * p.head_dim);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s0 + i < p.splits) o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), s0 + i)) * x[i];
   }
-  const bool none = parts[p.head_dim + 1] < 0.f;
   if (here) {
     alignas(16) T w[4];
 #pragma unroll
@@ -443,17 +450,34 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
   if (p.lse && lane == 0) p.lse[(long long)head * p.rows_q + row] = none ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Tiles whose numbers the rows of a band can have (see find_tile: a row's lies between floor(row group / kRows) - 1 and floor(...) + its sequence).
+// How a call is cut: which tiles the rows of a band can have (see find_tile: a row's number lies between floor(row group / kRows) - 1 and floor(...) + its
+// sequence), and parts of the keys: those with which the call is estimated to be done first. A workgroup takes `alone` us a tile of keys where it is alone on
+// its compute unit and `shared` where it is one of two; joining reads and writes the parts' outputs and is a launch. Measured with 1, 2, 4, 8, 16, 32 and 64
+// parts, us: a row of 32 heads (8 of keys) on 8 000 keys 144, 78, 44, 27, 19, 17, 21; 8 such rows on 4 000 keys 81, 52, 35, 34, 38, 46, 65; 256 rows on 4 000 keys 83,
+// 52, 35, 37, 49, 73, 137; a prompt of 1 000 rows 27, 41, 47, 67, ..; in fp32 with 12 heads (4) 138, 84, 74, 76, ...
 struct Cut { int tile0, tiles, splits; };
 Cut cut(const lop_attention_t* op, lop_rows_t rows) {
   const long long group = op->heads_q / op->heads_k;
   Cut c;
   c.tile0 = (int)std::max(rows.lo * group / kRows - 1, 0LL);
   c.tiles = (int)((rows.hi * group - 1) / kRows + op->seqs - c.tile0);
-  // Two workgroups fit a compute unit. Where there are fewer than that the keys are cut into parts of 256 at least.
-  const long long blocks = (long long)c.tiles * op->heads_k;
-  c.splits = (int)std::max(1LL, std::min({ceil_div(1024, blocks), (long long)op->max_keys / (LOP_ATTENTION_CUT / 2), 64LL}));
-  if (blocks >= 512) c.splits = 1;
+  c.splits = 1;
+  if (op->max_keys < LOP_ATTENTION_CUT) return c;
+  struct Price { int keys; double alone, shared; };   // (shared 0: a workgroup has its compute unit for itself)
+  static constexpr Price prices[2][4] = {{{64, 0.9, 1.2}, {64, 1.1, 1.7}, {64, 1.3, 2.0}, {64, 2.9, 0.0}},     // bf16: 64, 96, 128, 256 values a head
+                                         {{64, 4.4, 8.0}, {32, 3.0, 5.8}, {32, 4.0, 7.8}, {32, 8.0, 0.0}}};    // fp32
+  const Price& price = prices[op->dtype == LOP_F32][op->head_dim <= 64 ? 0 : op->head_dim <= 96 ? 1 : op->head_dim <= 128 ? 2 : 3];
+  constexpr double kCus = 256.0;
+  const double blocks = (double)c.tiles * op->heads_k, band = rows.hi - rows.lo, tiles = (double)ceil_div(op->max_keys, price.keys);
+  // (of a causal prompt the average row sees half of the keys)
+  const double seen = op->causal ? 1.0 - 0.5 * std::min(1.0, (double)op->rows_q / op->seqs / op->max_keys) : 1.0;
+  double least = 0.0;
+  for (int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+    const double each = std::ceil(tiles / s), units = blocks * s / kCus, full = price.shared > 0.0 ? units / 2 * price.shared : units * price.alone;
+    double time = units <= 1.0 ? each * price.alone : each * std::max(price.alone, seen * full);
+    if (s > 1) time += 5.0 + s * band * op->heads_q * op->head_dim * 8.0 / 3.5e6;
+    if (s == 1 || time < least) { c.splits = s; least = time; }
+  }
   return c;
 }
 unsigned long long workspace_of(const lop_attention_t* op, lop_rows_t rows, int splits) {
@@ -511,7 +535,7 @@ extern "C" int lop_attention(const lop_attention_t* op, lop_rows_t rows, void* s
   if (op->rows_k > 0 && (!good(op->k, op->k_token, op->k_head, op->rows_k, op->heads_k) || !good(op->v, op->v_token, op->v_head, op->rows_k, op->heads_k)))
     return LOP_ERR_INVALID_ARG;
   if (!op->q_offsets || !op->k_begin || !op->k_end) return LOP_ERR_INVALID_ARG;
-  if (((uintptr_t)op->q_offsets | (uintptr_t)op->k_begin | (uintptr_t)op->k_end | (uintptr_t)op->lse | (uintptr_t)op->workspace) & 3) return LOP_ERR_INVALID_ARG;
+  if (((uintptr_t)op->q_offsets | (uintptr_t)op->k_begin | (uintptr_t)op->k_end | (uintptr_t)op->lse) & 3 || !aligned16(op->workspace)) return LOP_ERR_INVALID_ARG;
   // (a tile's keys are one buffer: its rows lie behind one another, and offsets in it are 32 bits)
   if (op->rows_k > 1 && (op->k_token < op->head_dim || op->v_token < op->head_dim)) return LOP_ERR_INVALID_ARG;
   if (op->rows_k > 1 && (op->k_token * E > (1LL << 31) / 128 || op->v_token * E > (1LL << 31) / 128)) return LOP_ERR_UNSUPPORTED;

@@ -70,7 +70,7 @@ def attention_op():
 @pytest.mark.parametrize("code,rows,change", [
     (ARG, (0, 9), dict(q=None)), (ARG, (0, 9), dict(k=None)), (ARG, (0, 9), dict(v=None)), (ARG, (0, 9), dict(out=None)), (ARG, (0, 9), dict(q_offsets=None)),
     (ARG, (0, 9), dict(k_begin=None)), (ARG, (0, 9), dict(k_end=None)), (ARG, (0, 9), dict(q=A + 8)), (ARG, (0, 9), dict(v=A + 2)), (ARG, (0, 9), dict(k_end=A + 2)),
-    (ARG, (0, 9), dict(lse=A + 1)), (ARG, (0, 9), dict(workspace=A + 2)), (ARG, (0, 9), dict(q_token=100)), (ARG, (0, 9), dict(out_head=-64)), (ARG, (0, 9), dict(k_token=56)),
+    (ARG, (0, 9), dict(lse=A + 1)), (ARG, (0, 9), dict(workspace=A + 8)), (ARG, (0, 9), dict(q_token=100)), (ARG, (0, 9), dict(out_head=-64)), (ARG, (0, 9), dict(k_token=56)),
     (ARG, (0, 9), dict(v_token=0)), (ARG, (0, 9), dict(scale=0.0)), (ARG, (0, 9), dict(scale=-1.0)), (ARG, (0, 9), dict(scale=float("inf"))), (ARG, (0, 9), dict(scale=float("nan"))),
     (ARG, (0, 0), dict(heads_k=0)), (ARG, (0, 0), dict(seqs=-1)), (ARG, (0, 0), dict(rows_q=-1)), (ARG, (0, 0), dict(rows_k=-1)), (ARG, (0, 0), dict(max_keys=-1)),
     (ARG, (0, 0), dict(head_dim=0)), (UNS, (0, 9), dict(head_dim=60)), (UNS, (0, 9), dict(head_dim=264)), (UNS, (0, 9), dict(dtype=2)), (UNS, (0, 9), dict(k_token=1 << 24)),
