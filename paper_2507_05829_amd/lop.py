@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_longlong, c_size_t, c_uint, c_ulonglong, c_void_p
 from typing import List, Optional, Sequence, Tuple
 
@@ -187,11 +188,11 @@ def _load() -> ctypes.CDLL:
                                       POINTER(lop_loss_layer_t), c_double, c_double,
                                       POINTER(lop_two_party_stats_t)]),
         "lop_measure_ceilings": (c_int, [POINTER(lop_ceilings_t)]),
-        "lop_quantize_blocks": (c_int, [POINTER(lop_quantize_t), lop_rows_t, c_void_p]),
-        "lop_rowwise_f8": (c_int, [POINTER(lop_rowwise_f8_t), lop_rows_t, c_void_p]),
-        "lop_head_norm_rope": (c_int, [POINTER(lop_head_norm_rope_t), lop_rows_t, c_void_p]),
-        "lop_attention_workspace": (c_int, [POINTER(lop_attention_t), lop_rows_t, POINTER(c_ulonglong)]),
-        "lop_attention": (c_int, [POINTER(lop_attention_t), lop_rows_t, c_void_p]),
+        "lop_quantize_blocks": (c_int, [c_void_p, lop_rows_t, c_void_p]),
+        "lop_rowwise_f8": (c_int, [c_void_p, lop_rows_t, c_void_p]),
+        "lop_head_norm_rope": (c_int, [c_void_p, lop_rows_t, c_void_p]),
+        "lop_attention_workspace": (c_int, [c_void_p, lop_rows_t, POINTER(c_ulonglong)]),
+        "lop_attention": (c_int, [c_void_p, lop_rows_t, c_void_p]),
         "lop_debug_guard_check": (c_int, []),
         "lop_strerror": (c_char_p, [c_int]),
         "lop_last_hip_error": (c_int, []),
@@ -594,35 +595,24 @@ def _bad(name: str, what: str):
     raise ValueError(f"{name}: {what}")
 
 
-def _fits(name: str, t, dtype, device: int, grad: bool) -> None:
-    """The tensor is of this type, on this device, its values next to one another and no gradient is wanted of it."""
-    if t.dtype is not dtype:
-        _bad(name, f"{dtype} is wanted, not {t.dtype}")
-    if t.get_device() != device:
-        _bad(name, f"on {t.device}, not on the current device ({device})")
-    if grad and t.requires_grad:
-        _bad(name, "forward only, but the tensor wants a gradient")
-
-
-def _rows_of(name: str, t, dtype, device: int, grad: bool):
-    """The strides of a tensor that _fits, its values next to one another in a row."""
-    if t.dtype is not dtype or t.get_device() != device or (grad and t.requires_grad):
-        _fits(name, t, dtype, device, grad)
-    strides = t.stride()
-    if strides[-1] != 1 and t.shape[-1] > 1 and t.numel() > 0:
-        _bad(name, "the values of a row have to lie next to one another")
-    return strides
-
-
-def _shaped(name: str, t, shape) -> None:
-    if t.shape != shape:
-        _bad(name, f"{tuple(shape)} is wanted, not {tuple(t.shape)}")
-
-
-def _dims(name: str, t, n: int):
-    if t.dim() != n:
-        _bad(name, f"{n} dimensions are wanted, not {t.dim()}")
-    return t.shape
+def _refuse(device: int, grad: bool, *named) -> None:
+    """Says what is wrong with the first of (name, tensor, type, shape, rows) that does not fit: `shape` None for any, or with None
+    for any extent; `rows`: the values of a row lie next to one another (2: all of them do)."""
+    for name, t, dtype, shape, rows in named:
+        if t is None:
+            continue
+        if t.dtype is not dtype:
+            _bad(name, f"{dtype} is wanted, not {t.dtype}")
+        if shape is not None and (len(shape) != t.dim() or any(a is not None and a != b for a, b in zip(shape, t.shape))):
+            _bad(name, f"{tuple(shape)} is wanted, not {tuple(t.shape)}")
+        if t.get_device() != device:
+            _bad(name, f"on {t.device}, not on the current device ({device})")
+        if grad and t.requires_grad:
+            _bad(name, "forward only, but the tensor wants a gradient")
+        if rows == 2 and not t.is_contiguous():
+            _bad(name, "dense memory is wanted")
+        if rows and t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel() > 0:
+            _bad(name, "the values of a row have to lie next to one another")
 
 
 def _dtype(name: str, t: torch.Tensor) -> int:
@@ -630,6 +620,12 @@ def _dtype(name: str, t: torch.Tensor) -> int:
     if code is None:
         _bad(name, f"float32 or bfloat16 is wanted, not {t.dtype}")
     return code
+
+
+def _dims(name: str, t, n: int):
+    if t.dim() != n:
+        _bad(name, f"{n} dimensions are wanted, not {t.dim()}")
+    return t.shape
 
 
 def _band(rows, total: int) -> lop_rows_t:
@@ -642,28 +638,36 @@ def _here():
     return device, torch._C._cuda_getCurrentRawStream(device), torch.is_grad_enabled()
 
 
+# Each function first asks in one expression whether everything fits, and goes through the tensors one by one only where
+# something does not: a call of one token is bound by the host. (The descriptors are packed for the same reason:
+# filling the fields of a ctypes structure takes four times as long.)
+_QUANTIZE = struct.Struct("@4iPqPqP2q")
+_ROWWISE_F8 = struct.Struct("@5iPqP2qPqP2q2PqPq")
+_HEAD_NORM_ROPE = struct.Struct("@7i2fP2qP2qP2qP2q4P")
+_ATTENTION = struct.Struct("@9ifP2qP2qP2qP2q5PQ")
+
+
 def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
     """x (m, k) in e4m3 with a scale for each block of `block_rows` x 128 values (see lop_quantize_blocks). Returns
     (q, scale): q float8_e4m3fn (m, k), scale float32 (ceil(m / block_rows), ceil(k / 128)), allocated with the scales
     of a column of blocks next to one another."""
     device, stream, grad = _here()
-    dtype = _dtype("x", x)
-    m, k = _dims("x", x, 2)
+    code, shape = _dtype("x", x), _dims("x", x, 2)
+    m, k = shape
     if block_rows != 1 and block_rows != LOP_F8_BLOCK:
         _bad("block_rows", f"1 or {LOP_F8_BLOCK}")
-    shape = (-(-m // block_rows), -(-k // LOP_F8_BLOCK))
+    blocks = (-(-m // block_rows), -(-k // LOP_F8_BLOCK))
     if q is None:
         q = torch.empty((m, k), dtype=_F8, device=x.device)
     if scale is None:
-        scale = torch.empty(shape[::-1], dtype=torch.float32, device=x.device).t()
-    xs = _rows_of("x", x, x.dtype, device, grad)
-    qs = _rows_of("q", q, _F8, device, grad)
-    _fits("scale", scale, torch.float32, device, grad)
-    _shaped("q", q, x.shape)
-    _shaped("scale", scale, shape)
-    s0, s1 = scale.stride()
-    op = lop_quantize_t(m, k, dtype, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), s0, s1)
-    _check(_lib.lop_quantize_blocks(byref(op), _band(rows, m), stream), "lop_quantize_blocks")
+        scale = torch.empty(blocks[::-1], dtype=torch.float32, device=x.device).t()
+    xs, qs, ss = x.stride(), q.stride(), scale.stride()
+    if (q.dtype is not _F8 or scale.dtype is not torch.float32 or q.shape != shape or scale.shape != blocks
+            or x.get_device() != device or q.get_device() != device or scale.get_device() != device
+            or (grad and (x.requires_grad or q.requires_grad or scale.requires_grad)) or xs[1] != 1 or qs[1] != 1):
+        _refuse(device, grad, ("x", x, x.dtype, None, 1), ("q", q, _F8, shape, 1), ("scale", scale, torch.float32, blocks, 0))
+    op = _QUANTIZE.pack(m, k, code, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), ss[0], ss[1])
+    _check(_lib.lop_quantize_blocks(op, _band(rows, m), stream), "lop_quantize_blocks")
     return q, scale
 
 
@@ -679,31 +683,25 @@ def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=No
     if y is None:
         y = torch.empty((m, n), dtype=dtype or torch.bfloat16, device=x.device)
     code, dtype, f32 = _dtype("y", y), y.dtype, torch.float32
-    if kw != k:
-        _bad("w", f"{k} columns are wanted, not {kw}")
-    xs = _rows_of("x", x, _F8, device, grad)
-    ws = _rows_of("w", w, _F8, device, grad)
-    _fits("x_scale", x_scale, f32, device, grad)
-    _fits("w_scale", w_scale, f32, device, grad)
-    ys = _rows_of("y", y, dtype, device, grad)
-    _shaped("x_scale", x_scale, (m, kb))
-    _shaped("w_scale", w_scale, (-(-n // LOP_F8_BLOCK), kb))
-    _shaped("y", y, (m, n))
-    bias_at = residual_at = None
-    residual_stride = 0
+    xs, ws, ys, xss, wss = x.stride(), w.stride(), y.stride(), x_scale.stride(), w_scale.stride()
+    if (x.dtype is not _F8 or w.dtype is not _F8 or x_scale.dtype is not f32 or w_scale.dtype is not f32 or kw != k
+            or x_scale.shape != (m, kb) or w_scale.shape != (-(-n // LOP_F8_BLOCK), kb) or y.shape != (m, n)
+            or x.get_device() != device or w.get_device() != device or x_scale.get_device() != device
+            or w_scale.get_device() != device or y.get_device() != device
+            or (grad and (x.requires_grad or w.requires_grad or x_scale.requires_grad or w_scale.requires_grad or y.requires_grad))
+            or xs[1] != 1 or ws[1] != 1 or ys[1] != 1):
+        _refuse(device, grad, ("x", x, _F8, None, 1), ("w", w, _F8, (n, k), 1), ("x_scale", x_scale, f32, (m, kb), 0),
+                ("w_scale", w_scale, f32, (-(-n // LOP_F8_BLOCK), kb), 0), ("y", y, dtype, (m, n), 1))
+    bias_at = residual_at = residual_stride = 0
     if bias is not None:
-        _rows_of("bias", bias, f32, device, grad)
-        _shaped("bias", bias, (n,))
+        _refuse(device, grad, ("bias", bias, f32, (n,), 1))
         bias_at = bias.data_ptr()
     if residual is not None:
-        residual_stride = _rows_of("residual", residual, dtype, device, grad)[0]
-        _shaped("residual", residual, (m, n))
-        residual_at = residual.data_ptr()
-    xs0, xs1 = x_scale.stride()
-    ws0, ws1 = w_scale.stride()
-    op = lop_rowwise_f8_t(m, n, k, code, _ACTS[act], x.data_ptr(), xs[0], x_scale.data_ptr(), xs0, xs1, w.data_ptr(), ws[0],
-                          w_scale.data_ptr(), ws0, ws1, bias_at, residual_at, residual_stride, y.data_ptr(), ys[0])
-    _check(_lib.lop_rowwise_f8(byref(op), _band(rows, m), stream), "lop_rowwise_f8")
+        _refuse(device, grad, ("residual", residual, dtype, (m, n), 1))
+        residual_at, residual_stride = residual.data_ptr(), residual.stride(0)
+    op = _ROWWISE_F8.pack(m, n, k, code, _ACTS[act], x.data_ptr(), xs[0], x_scale.data_ptr(), xss[0], xss[1], w.data_ptr(), ws[0],
+                          w_scale.data_ptr(), wss[0], wss[1], bias_at, residual_at, residual_stride, y.data_ptr(), ys[0])
+    _check(_lib.lop_rowwise_f8(op, _band(rows, m), stream), "lop_rowwise_f8")
     return y
 
 
@@ -713,42 +711,51 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
     2 * len(freq) values rotated by positions * freq (see lop_head_norm_rope). positions int32 (tokens,), freq float32,
     both None for no rotation. Returns (q_out, k_out), which may be q and k."""
     device, stream, grad = _here()
-    code, dtype, f32 = _dtype("q", q), q.dtype, torch.float32
-    tokens, hq, d = _dims("q", q, 3)
+    code, dtype, f32, shape = _dtype("q", q), q.dtype, torch.float32, _dims("q", q, 3)
+    tokens, hq, d = shape
     if q_out is None:
-        q_out = torch.empty((tokens, hq, d), dtype=dtype, device=q.device)
-    qs = _rows_of("q", q, dtype, device, grad)
-    qos = _rows_of("q_out", q_out, dtype, device, grad)
-    _shaped("q_out", q_out, q.shape)
-    hk, k_at, k_out_at, ks, kos = 0, None, None, (0, 0), (0, 0)
+        q_out = torch.empty(shape, dtype=dtype, device=q.device)
+    qs, qos = q.stride(), q_out.stride()
+    if (q_out.dtype is not dtype or q_out.shape != shape or q.get_device() != device or q_out.get_device() != device
+            or (grad and (q.requires_grad or q_out.requires_grad)) or qs[2] != 1 or qos[2] != 1):
+        _refuse(device, grad, ("q", q, dtype, None, 1), ("q_out", q_out, dtype, shape, 1))
+    hk = k_at = k_out_at = 0
+    ks = kos = (0, 0)
     if k is not None:
-        hk = _dims("k", k, 3)[1]
+        k_shape = _dims("k", k, 3)
+        hk = k_shape[1]
         if k_out is None:
-            k_out = torch.empty((tokens, hk, d), dtype=dtype, device=q.device)
-        ks = _rows_of("k", k, dtype, device, grad)
-        kos = _rows_of("k_out", k_out, dtype, device, grad)
-        _shaped("k", k, (tokens, hk, d))
-        _shaped("k_out", k_out, k.shape)
+            k_out = torch.empty(k_shape, dtype=dtype, device=q.device)
+        ks, kos = k.stride(), k_out.stride()
+        if (k.dtype is not dtype or k_out.dtype is not dtype or k_shape[0] != tokens or k_shape[2] != d or k_out.shape != k_shape
+                or k.get_device() != device or k_out.get_device() != device or (grad and (k.requires_grad or k_out.requires_grad))
+                or ks[2] != 1 or kos[2] != 1):
+            _refuse(device, grad, ("k", k, dtype, (tokens, hk, d), 1), ("k_out", k_out, dtype, k_shape, 1))
         k_at, k_out_at = k.data_ptr(), k_out.data_ptr()
-    if (positions is None) != (freq is None):
-        _bad("positions", "they and freq go together")
-    turns, positions_at, freq_at = 0, None, None
-    if freq is not None:
-        _rows_of("positions", positions, torch.int32, device, grad)
-        _rows_of("freq", freq, f32, device, grad)
-        turns = _dims("freq", freq, 1)[0]
-        _shaped("positions", positions, (tokens,))
+    turns = positions_at = freq_at = q_weight_at = k_weight_at = 0
+    if freq is not None and positions is not None:
+        turns = freq.numel()
+        if (positions.dtype is not torch.int32 or freq.dtype is not f32 or freq.dim() != 1 or positions.shape != (tokens,)
+                or positions.get_device() != device or freq.get_device() != device or freq.requires_grad
+                or positions.stride(0) != 1 or freq.stride(0) != 1):
+            _refuse(device, grad, ("positions", positions, torch.int32, (tokens,), 1), ("freq", freq, f32, (None,), 1))
         positions_at, freq_at = positions.data_ptr(), freq.data_ptr()
-    weights = [None, None]
-    for i, t in enumerate((q_weight, k_weight)):
-        if t is not None:
-            _rows_of("weight", t, f32, device, grad)
-            _shaped("weight", t, (d,))
-            weights[i] = t.data_ptr()
-    op = lop_head_norm_rope_t(tokens, hq, hk, d, 2 * turns, interleaved, code, eps, amplitude, q.data_ptr(), qs[0], qs[1],
+    elif freq is not None or positions is not None:
+        _bad("positions", "they and freq go together")
+    if q_weight is not None:
+        if (q_weight.dtype is not f32 or q_weight.shape != (d,) or q_weight.get_device() != device or q_weight.requires_grad
+                or q_weight.stride(0) != 1):
+            _refuse(device, grad, ("q_weight", q_weight, f32, (d,), 1))
+        q_weight_at = q_weight.data_ptr()
+    if k_weight is not None:
+        if (k_weight.dtype is not f32 or k_weight.shape != (d,) or k_weight.get_device() != device or k_weight.requires_grad
+                or k_weight.stride(0) != 1):
+            _refuse(device, grad, ("k_weight", k_weight, f32, (d,), 1))
+        k_weight_at = k_weight.data_ptr()
+    op = _HEAD_NORM_ROPE.pack(tokens, hq, hk, d, 2 * turns, interleaved, code, eps, amplitude, q.data_ptr(), qs[0], qs[1],
                               k_at, ks[0], ks[1], q_out.data_ptr(), qos[0], qos[1], k_out_at, kos[0], kos[1],
-                              weights[0], weights[1], positions_at, freq_at)
-    _check(_lib.lop_head_norm_rope(byref(op), _band(rows, tokens), stream), "lop_head_norm_rope")
+                              q_weight_at, k_weight_at, positions_at, freq_at)
+    _check(_lib.lop_head_norm_rope(op, _band(rows, tokens), stream), "lop_head_norm_rope")
     return q_out, k_out
 
 
@@ -759,46 +766,39 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
     sequence as far as known (None: all of k), lse: float32 (heads_q, rows_q) or None, workspace: uint8 of
     lop_attention_workspace bytes (None: allocated). Returns out."""
     device, stream, grad = _here()
-    code, dtype, i32 = _dtype("q", q), q.dtype, torch.int32
-    rows_q, hq, d = _dims("q", q, 3)
-    rows_k, hk, _ = _dims("k", k, 3)
+    code, dtype, i32, shape, k_shape = _dtype("q", q), q.dtype, torch.int32, _dims("q", q, 3), _dims("k", k, 3)
+    rows_q, hq, d = shape
+    rows_k, hk, _ = k_shape
     seqs = _dims("k_begin", k_begin, 1)[0]
     if out is None:
-        out = torch.empty((rows_q, hq, d), dtype=dtype, device=q.device)
-    qs = _rows_of("q", q, dtype, device, grad)
-    ks = _rows_of("k", k, dtype, device, grad)
-    vs = _rows_of("v", v, dtype, device, grad)
-    os_ = _rows_of("out", out, dtype, device, grad)
-    _rows_of("q_offsets", q_offsets, i32, device, grad)
-    _rows_of("k_begin", k_begin, i32, device, grad)
-    _rows_of("k_end", k_end, i32, device, grad)
-    _shaped("k", k, (rows_k, hk, d))
-    _shaped("v", v, k.shape)
-    _shaped("out", out, q.shape)
-    _shaped("q_offsets", q_offsets, (seqs + 1,))
-    _shaped("k_end", k_end, (seqs,))
-    lse_at = None
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), out.stride()
+    if (k.dtype is not dtype or v.dtype is not dtype or out.dtype is not dtype or q_offsets.dtype is not i32 or k_begin.dtype is not i32
+            or k_end.dtype is not i32 or k_shape[2] != d or v.shape != k_shape or out.shape != shape or q_offsets.shape != (seqs + 1,)
+            or k_end.shape != (seqs,) or q.get_device() != device or k.get_device() != device or v.get_device() != device
+            or out.get_device() != device or q_offsets.get_device() != device or k_begin.get_device() != device
+            or k_end.get_device() != device or (grad and (q.requires_grad or k.requires_grad or v.requires_grad or out.requires_grad))
+            or qs[2] != 1 or ks[2] != 1 or vs[2] != 1 or os_[2] != 1 or q_offsets.stride(0) != 1 or k_begin.stride(0) != 1
+            or k_end.stride(0) != 1):
+        _refuse(device, grad, ("q", q, dtype, None, 1), ("k", k, dtype, (rows_k, hk, d), 1), ("v", v, dtype, k_shape, 1),
+                ("out", out, dtype, shape, 1), ("q_offsets", q_offsets, i32, (seqs + 1,), 1), ("k_begin", k_begin, i32, (seqs,), 1),
+                ("k_end", k_end, i32, (seqs,), 1))
+    lse_at = workspace_at = workspace_bytes = 0
     if lse is not None:
-        _fits("lse", lse, torch.float32, device, grad)
-        _shaped("lse", lse, (hq, rows_q))
-        if not lse.is_contiguous():
-            _bad("lse", "dense rows are wanted")
+        _refuse(device, grad, ("lse", lse, torch.float32, (hq, rows_q), 2))
         lse_at = lse.data_ptr()
     if max_keys is None:
         max_keys = rows_k
-    op = lop_attention_t(code, hq, hk, d, seqs, rows_q, rows_k, max_keys, causal, scale,
-                         q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1], v.data_ptr(), vs[0], vs[1],
-                         out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), lse_at, None, 0)
     band = _band(rows, rows_q)
+    fields = (code, hq, hk, d, seqs, rows_q, rows_k, max_keys, causal, scale, q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1],
+              v.data_ptr(), vs[0], vs[1], out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), lse_at)
     if workspace is None and max_keys >= LOP_ATTENTION_CUT:
         n = c_ulonglong(0)
-        _check(_lib.lop_attention_workspace(byref(op), band, byref(n)), "lop_attention_workspace")
+        _check(_lib.lop_attention_workspace(_ATTENTION.pack(*fields, 0, 0), band, byref(n)), "lop_attention_workspace")
         if n.value:
             workspace = torch.empty(n.value, dtype=torch.uint8, device=q.device)
     if workspace is not None:
-        _fits("workspace", workspace, torch.uint8, device, grad)
-        if not workspace.is_contiguous():
-            _bad("workspace", "dense memory is wanted")
-        op.workspace, op.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(_lib.lop_attention(byref(op), band, stream), "lop_attention")
+        _refuse(device, grad, ("workspace", workspace, torch.uint8, (None,), 2))
+        workspace_at, workspace_bytes = workspace.data_ptr(), workspace.numel()
+    _check(_lib.lop_attention(_ATTENTION.pack(*fields, workspace_at, workspace_bytes), band, stream), "lop_attention")
     return out

@@ -1,5 +1,7 @@
 """The transformer operators without a GPU: what the library refuses, sizes of workspaces, and the pins of their plain 64-bit
 forms against third-party routines and closed forms. No kernel is launched."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -77,6 +79,15 @@ def attention_op():
     (UNS, (0, 9), dict(rows_q=(1 << 31) - 1)), (SHAPE, (0, 9), dict(heads_q=5)), (BAND, (0, 51), {}), (BAND, (-1, 9), {}), (BAND, (9, 8), {})])
 def test_attention_refuses(code, rows, change):
     refused(lop.lop_attention, attention_op(), rows, code, **change)
+
+
+def test_packed_descriptors_are_the_structures():
+    for packed, structure in ((lop._QUANTIZE, lop.lop_quantize_t), (lop._ROWWISE_F8, lop.lop_rowwise_f8_t),
+                              (lop._HEAD_NORM_ROPE, lop.lop_head_norm_rope_t), (lop._ATTENTION, lop.lop_attention_t)):
+        assert packed.size == ctypes.sizeof(structure)
+        values = [i + 1 for i in range(len(structure._fields_))]
+        op = structure.from_buffer_copy(packed.pack(*values))
+        assert [getattr(op, name) for name, _ in structure._fields_] == values
 
 
 def test_empty_bands_enqueue_nothing():
