@@ -58,7 +58,8 @@ __global__ __launch_bounds__(256) void head_norm_rope_kernel(const RopeParams p)
   constexpr int SIDE = 64 / LANES;   // heads side by side
   const int lane = threadIdx.x & 63, j = lane % LANES, side = lane / LANES;
   const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int token = p.lo + (int)(wave / p.parts), part = (int)(wave % p.parts);
+  const long long token = p.lo + wave / p.parts;
+  const int part = (int)(wave % p.parts);
   if (token >= p.hi) return;   // (no barrier follows)
   const bool live = j * 8 < p.head_dim;
   const bool turns = j * 8 < p.rot_dim;
@@ -185,6 +186,10 @@ extern "C" int lop_head_norm_rope(const lop_head_norm_rope_t* op, lop_rows_t row
   if (!good(op->q, op->q_token, op->q_head, op->heads_q) || !good(op->q_out, op->q_out_token, op->q_out_head, op->heads_q) ||
       !good(op->k, op->k_token, op->k_head, op->heads_k) || !good(op->k_out, op->k_out_token, op->k_out_head, op->heads_k))
     return LOP_ERR_INVALID_ARG;
+  for (int i = 0; i < 2; ++i)   // an output's heads do not overlap
+    if (const int heads = i ? op->heads_k : op->heads_q; heads > 0 && (!apart(i ? op->k_out_token : op->q_out_token, op->head_dim, op->tokens) ||
+                                                                      !apart(i ? op->k_out_head : op->q_out_head, op->head_dim, heads)))
+      return LOP_ERR_INVALID_ARG;
   if (!aligned16(op->q_weight) || !aligned16(op->k_weight)) return LOP_ERR_INVALID_ARG;
   if (op->rot_dim > 0 && (!op->positions || ((uintptr_t)op->positions & 3) || !op->freq || !aligned16(op->freq))) return LOP_ERR_INVALID_ARG;
   if ((op->q_weight || op->k_weight) && !(op->eps >= 0.f)) return LOP_ERR_INVALID_ARG;

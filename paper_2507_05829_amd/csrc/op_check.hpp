@@ -16,6 +16,8 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 inline bool whole_vectors(long long stride, size_t element, bool used) {
   return !used || (stride >= 0 && (size_t)stride * element % 16 == 0);
 }
+// Rows (or heads) of an output of `extent` elements do not overlap.
+inline bool apart(long long stride, long long extent, long long count) { return count <= 1 || stride >= extent; }
 inline size_t dtype_bytes(int dtype) { return dtype == LOP_BF16 ? 2 : 4; }
 inline bool known_dtype(int dtype) { return dtype == LOP_F32 || dtype == LOP_BF16; }
 // LOP_OK, or what a band that is no interval of `total` rows is

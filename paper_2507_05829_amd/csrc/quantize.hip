@@ -66,7 +66,8 @@ __global__ __launch_bounds__(256) void quantize_kernel(const QuantizeParams p) {
   constexpr int TILE = 16 * ROWS;
   const int tile = blockIdx.x / p.blocks, kb = blockIdx.x - tile * p.blocks;
   const int group = threadIdx.x >> 4, lane = threadIdx.x & 15;
-  const int row0 = p.lo + tile * TILE + group * ROWS, col = kb * kBlock + lane * 8;
+  const long long row0 = p.lo + (long long)tile * TILE + group * ROWS;
+  const int col = kb * kBlock + lane * 8;
   Eight<T> in[ROWS];
 #pragma unroll
   for (int i = 0; i < ROWS; ++i) {
@@ -144,6 +145,8 @@ extern "C" int lop_quantize_blocks(const lop_quantize_t* op, lop_rows_t rows, vo
   if (op->block_rows != 1 && (rows.lo % kBlock || (rows.hi % kBlock && rows.hi != op->m))) return LOP_ERR_BAND_RANGE;
   if (rows.lo == rows.hi) return LOP_OK;
   if (!op->x || !op->q || !op->scale || !aligned16(op->x) || !aligned16(op->q) || ((uintptr_t)op->scale & 3)) return LOP_ERR_INVALID_ARG;
-  if (!whole_vectors(op->x_stride, dtype_bytes(op->dtype), op->m > 1) || !whole_vectors(op->q_stride, 1, op->m > 1)) return LOP_ERR_INVALID_ARG;
+  if (!whole_vectors(op->x_stride, dtype_bytes(op->dtype), op->m > 1) || !whole_vectors(op->q_stride, 1, op->m > 1) || !apart(op->q_stride, op->k, op->m))
+    return LOP_ERR_INVALID_ARG;
+  if (op->scale_row < 0 || op->scale_col < 0) return LOP_ERR_INVALID_ARG;
   return op->dtype == LOP_BF16 ? quantize<__bf16>(op, rows, (hipStream_t)stream) : quantize<float>(op, rows, (hipStream_t)stream);
 }

@@ -643,6 +643,7 @@ extern "C" int lop_rowwise_f8(const lop_rowwise_f8_t* op, lop_rows_t rows, void*
   if (!op->x || !op->w || !op->x_scale || !op->w_scale || !op->y || !aligned16(op->x) || !aligned16(op->w)) return LOP_ERR_INVALID_ARG;
   if (((uintptr_t)op->x_scale | (uintptr_t)op->w_scale | (uintptr_t)op->bias) & 3) return LOP_ERR_INVALID_ARG;
   if (((uintptr_t)op->y | (uintptr_t)op->residual) & (E - 1)) return LOP_ERR_INVALID_ARG;
+  if (!apart(op->y_stride, op->n, op->m)) return LOP_ERR_INVALID_ARG;
   if (!whole_vectors(op->x_stride, 1, op->m > 1) || !whole_vectors(op->w_stride, 1, op->n > 1)) return LOP_ERR_INVALID_ARG;
   if (op->x_scale_row < 0 || op->x_scale_col < 0 || op->w_scale_row < 0 || op->w_scale_col < 0 || op->y_stride < 0 ||
       (op->residual && op->residual_stride < 0))

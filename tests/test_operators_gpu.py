@@ -327,6 +327,61 @@ def test_attention_offsets_outside_are_cut_off():
     assert (out[10:] == 99).all()
 
 
+# ------------------------------------------------------------------ far into large tensors
+
+def test_offsets_that_pass_32_bits():
+    """The last rows of tensors of more than 4 GiB, of which only those are filled."""
+    rng = np.random.default_rng(13)
+    m, k, n, lo = 1100000, 4096, 48, 1099960
+    x, xs, w, ws = operands(rng, m - lo, k, n)
+    big, scales = torch.empty(m, k, dtype=F8, device="cuda"), torch.empty(32, m, device="cuda").t()
+    big[lo:], scales[lo:] = dev(x).to(F8), dev(xs)
+    y = lop.rowwise_f8(big, scales, dev(w).to(F8), dev(ws), rows=(lo, m))
+    want, size = plain.product(x, xs, w, ws)
+    assert_near(host(y[lo:]), want, product_tolerance(want, size, k, "bf16"), "product")
+    values_in = values(rng, (m - lo, k), "bf16")
+    wide = torch.empty(m, k, dtype=torch.bfloat16, device="cuda")
+    wide[lo:] = dev(values_in, "bf16")
+    lop.quantize_blocks(wide, q=big, scale=scales, rows=(lo, m))
+    want_q, want_s = plain.quantize(values_in, 1)
+    np.testing.assert_array_equal(host(big[lo:]), want_q)
+    np.testing.assert_array_equal(host(scales[lo:]), want_s)
+    del big
+    pos, freq = torch.arange(m, dtype=torch.int32, device="cuda"), (1e4 ** (-np.arange(32) / 32.0)).astype(np.float32)
+    heads = wide.view(m, 32, 128)
+    lop.head_norm_rope(heads, None, pos, dev(freq), q_out=heads, rows=(lo, m))
+    want, size = plain.norm_rope(values_in.reshape(-1, 32, 128), np.arange(lo, m), freq, None, 0.0, False, 1.0)
+    assert_near(host(heads[lo:]), want, rope_tolerance(want, size, 128, "bf16"), "rotation")
+    q, v = values(rng, (3, 32, 128), "bf16"), values(rng, (m - lo, 32, 128), "bf16")
+    cache = torch.empty(m, 32, 128, dtype=torch.bfloat16, device="cuda")
+    cache[lo:] = dev(v, "bf16")
+    i32 = lambda a: dev(np.array(a, np.int32))  # noqa: E731
+    out = lop.attention(dev(q, "bf16"), heads, cache, i32([0, 3]), i32([lo]), i32([m]), 0.1)
+    want, _, size, spread = plain.attention(q, host(heads[lo:]), v, [0, 3], [0], [m - lo], 0.1, True)
+    assert_near(host(out), want, attention_tolerance(want, size, spread, m - lo, 128, "bf16"), "attention")
+
+
+def test_a_cache_longer_than_its_bytes_fit_32_bits():
+    """One sequence of which the last key lies more than 4 GiB behind the first; nearly all weight lies on a few keys."""
+    rng = np.random.default_rng(14)
+    n, d = 70000, 128
+    kv = torch.zeros(n, 256, d, dtype=torch.bfloat16, device="cuda")     # one key head of 256: 64 KiB from key to key
+    k, v = kv[:, :1], kv[:, 1:2]
+    q = values(rng, (1, 1, d), "bf16")
+    v[:] = 1.0
+    spikes = [3, 32767, 32768, 65535, 65536, n - 1]
+    vals = values(rng, (len(spikes), d), "bf16")
+    for i, s in enumerate(spikes):
+        k[s, 0], v[s, 0] = dev(q[0, 0], "bf16"), dev(vals[i], "bf16")
+    scale = 40.0 / float((q[0, 0] ** 2).sum())                            # the others have weights of e^-40
+    i32 = lambda a: dev(np.array(a, np.int32))  # noqa: E731
+    for max_keys in (0, n):
+        out = lop.attention(dev(q, "bf16"), k, v, i32([0, 1]), i32([0]), i32([n]), scale, max_keys=max_keys)
+        want = vals.astype(np.float64).mean(0)[None, None]
+        # the others' weight, n e^-40 < 1e-12; weights and output rounded to bf16, sums of a few values of size up to 4
+        assert_near(host(out), want, 2 * 2.0 ** -8 * np.abs(vals).mean(0) + 1e-5, "spikes")
+
+
 # ------------------------------------------------------------------ streams, graphs, all together
 
 def test_operators_on_another_stream_and_in_a_graph():

@@ -28,7 +28,7 @@ def quantize_op():
 
 @pytest.mark.parametrize("code,rows,change", [
     (ARG, (0, 9), dict(x=None)), (ARG, (0, 9), dict(q=None)), (ARG, (0, 9), dict(scale=None)), (ARG, (0, 9), dict(x=A + 8)), (ARG, (0, 9), dict(q=A + 4)),
-    (ARG, (0, 9), dict(scale=A + 2)), (ARG, (0, 9), dict(x_stride=260)), (ARG, (0, 9), dict(q_stride=-256)), (ARG, (0, 9), dict(q_stride=264)),
+    (ARG, (0, 9), dict(scale=A + 2)), (ARG, (0, 9), dict(x_stride=260)), (ARG, (0, 9), dict(q_stride=-256)), (ARG, (0, 9), dict(q_stride=264)), (ARG, (0, 9), dict(q_stride=240)), (ARG, (0, 9), dict(scale_row=-1)),
     (ARG, (0, 0), dict(m=-1)), (ARG, (0, 0), dict(k=0)), (UNS, (0, 9), dict(k=250)), (UNS, (0, 9), dict(dtype=2)), (UNS, (0, 9), dict(block_rows=64)),
     (BAND, (-1, 9), {}), (BAND, (9, 8), {}), (BAND, (0, 201), {}), (BAND, (64, 200), dict(block_rows=128)), (BAND, (0, 100), dict(block_rows=128))])
 def test_quantize_refuses(code, rows, change):
@@ -43,7 +43,7 @@ def product_op():
     (ARG, (0, 9), dict(x=None)), (ARG, (0, 9), dict(w=None)), (ARG, (0, 9), dict(x_scale=None)), (ARG, (0, 9), dict(w_scale=None)), (ARG, (0, 9), dict(y=None)),
     (ARG, (0, 9), dict(x=A + 8)), (ARG, (0, 9), dict(w=A + 1)), (ARG, (0, 9), dict(y=A + 1)), (ARG, (0, 9), dict(residual=A + 1, residual_stride=60)),
     (ARG, (0, 9), dict(bias=A + 2)), (ARG, (0, 9), dict(x_scale=A + 1)), (ARG, (0, 9), dict(x_stride=257)), (ARG, (0, 9), dict(w_stride=-16)),
-    (ARG, (0, 9), dict(y_stride=-60)), (ARG, (0, 9), dict(x_scale_row=-1)), (ARG, (0, 9), dict(w_scale_col=-1)), (ARG, (0, 9), dict(n=0)), (ARG, (0, 0), dict(k=0)),
+    (ARG, (0, 9), dict(y_stride=-60)), (ARG, (0, 9), dict(y_stride=59)), (ARG, (0, 9), dict(x_scale_row=-1)), (ARG, (0, 9), dict(w_scale_col=-1)), (ARG, (0, 9), dict(n=0)), (ARG, (0, 0), dict(k=0)),
     (UNS, (0, 9), dict(k=100)), (UNS, (0, 9), dict(dtype=7)), (UNS, (0, 9), dict(act=3)), (UNS, (0, 9), dict(act=-1)), (UNS, (0, 9), dict(x_stride=1 << 24)),
     (UNS, (0, 9), dict(w_stride=1 << 24)), (UNS, (0, 9), dict(x_scale_row=1 << 24)), (UNS, (0, 9), dict(k=1 << 24)), (BAND, (0, 101), {}), (BAND, (5, 4), {}), (BAND, (-2, 4), {})])
 def test_product_refuses(code, rows, change):
@@ -57,7 +57,7 @@ def rope_op():
 @pytest.mark.parametrize("code,rows,change", [
     (ARG, (0, 9), dict(q=None)), (ARG, (0, 9), dict(k=None)), (ARG, (0, 9), dict(q_out=None)), (ARG, (0, 9), dict(k_out=None)), (ARG, (0, 9), dict(positions=None)),
     (ARG, (0, 9), dict(freq=None)), (ARG, (0, 9), dict(q=A + 8)), (ARG, (0, 9), dict(k_out=A + 2)), (ARG, (0, 9), dict(q_weight=A + 4)), (ARG, (0, 9), dict(freq=A + 4)),
-    (ARG, (0, 9), dict(positions=A + 1)), (ARG, (0, 9), dict(q_head=60)), (ARG, (0, 9), dict(k_token=-128)), (ARG, (0, 9), dict(eps=-1.0)), (ARG, (0, 9), dict(eps=float("nan"))),
+    (ARG, (0, 9), dict(positions=A + 1)), (ARG, (0, 9), dict(q_head=60)), (ARG, (0, 9), dict(k_token=-128)), (ARG, (0, 9), dict(q_out_head=56)), (ARG, (0, 9), dict(k_out_token=0)), (ARG, (0, 9), dict(eps=-1.0)), (ARG, (0, 9), dict(eps=float("nan"))),
     (ARG, (0, 0), dict(heads_q=0, heads_k=0)), (ARG, (0, 0), dict(heads_k=-1)), (ARG, (0, 0), dict(tokens=-1)), (ARG, (0, 0), dict(head_dim=0)), (ARG, (0, 0), dict(rot_dim=-8)),
     (UNS, (0, 9), dict(head_dim=60)), (UNS, (0, 9), dict(head_dim=264)), (UNS, (0, 9), dict(rot_dim=12)), (UNS, (0, 9), dict(dtype=3)), (SHAPE, (0, 9), dict(rot_dim=72)),
     (BAND, (0, 51), {}), (BAND, (-1, 3), {}), (BAND, (3, 2), {})])
@@ -72,7 +72,7 @@ def attention_op():
 @pytest.mark.parametrize("code,rows,change", [
     (ARG, (0, 9), dict(q=None)), (ARG, (0, 9), dict(k=None)), (ARG, (0, 9), dict(v=None)), (ARG, (0, 9), dict(out=None)), (ARG, (0, 9), dict(q_offsets=None)),
     (ARG, (0, 9), dict(k_begin=None)), (ARG, (0, 9), dict(k_end=None)), (ARG, (0, 9), dict(q=A + 8)), (ARG, (0, 9), dict(v=A + 2)), (ARG, (0, 9), dict(k_end=A + 2)),
-    (ARG, (0, 9), dict(lse=A + 1)), (ARG, (0, 9), dict(workspace=A + 8)), (ARG, (0, 9), dict(q_token=100)), (ARG, (0, 9), dict(out_head=-64)), (ARG, (0, 9), dict(k_token=56)),
+    (ARG, (0, 9), dict(lse=A + 1)), (ARG, (0, 9), dict(workspace=A + 8)), (ARG, (0, 9), dict(q_token=100)), (ARG, (0, 9), dict(out_head=-64)), (ARG, (0, 9), dict(out_head=0)), (ARG, (0, 9), dict(out_token=56)), (ARG, (0, 9), dict(k_token=56)),
     (ARG, (0, 9), dict(v_token=0)), (ARG, (0, 9), dict(scale=0.0)), (ARG, (0, 9), dict(scale=-1.0)), (ARG, (0, 9), dict(scale=float("inf"))), (ARG, (0, 9), dict(scale=float("nan"))),
     (ARG, (0, 0), dict(heads_k=0)), (ARG, (0, 0), dict(seqs=-1)), (ARG, (0, 0), dict(rows_q=-1)), (ARG, (0, 0), dict(rows_k=-1)), (ARG, (0, 0), dict(max_keys=-1)),
     (ARG, (0, 0), dict(head_dim=0)), (UNS, (0, 9), dict(head_dim=60)), (UNS, (0, 9), dict(head_dim=264)), (UNS, (0, 9), dict(dtype=2)), (UNS, (0, 9), dict(k_token=1 << 24)),
