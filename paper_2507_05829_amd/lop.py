@@ -5,7 +5,8 @@ library is not built, importing this module raises.
 Module-level functions carry the C names (lop_plan, lop_run_band, lop_run_chain, ...);
 ``Plan`` is a small convenience wrapper over the same calls. Device and pinned-host
 buffers are torch tensors used purely as memory; their ``data_ptr()`` is what crosses the
-boundary.
+boundary. ``quantize_blocks``, ``rowwise_f8``, ``head_norm_rope`` and ``attention`` are the calls of
+the same names on torch tensors, whose types, shapes and strides they pass on.
 """
 from __future__ import annotations
 
