@@ -17,6 +17,7 @@
 #include <cmath>
 
 #include "conv_common.hpp"
+#include "conv_split.hpp"
 #include "launch.hpp"
 #include "lop.h"
 #include "op_check.hpp"
@@ -67,6 +68,11 @@ __device__ __forceinline__ Place find_tile(const AttnParams& p, int t) {
   return Place{at < 0 ? -1 : lo, at};
 }
 
+// Of 16 lanes, lane i gets value i % 4 of the four that lanes i / 4, i / 4 + 4, + 8 and + 12 point at.
+__device__ __forceinline__ u32x2 transposed_read(const unsigned char* at) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)at));
+}
+
 __device__ __forceinline__ float max_of_halves(float v) {
   const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return __builtin_elementwise_maximum(__uint_as_float((unsigned)s[0]), __uint_as_float((unsigned)s[1]));
@@ -105,6 +111,9 @@ struct AttnShape {
   static constexpr int LD = BYTES / 4096;                // load instructions of a wavefront for one tile of either
   static constexpr int KS = DP * E / 32;                 // operands of a row: steps of 16 bytes in either half
   static constexpr int DT = DP / 32;
+  static constexpr bool PARTS = E == 4 && DP <= 128;     // (of 256 values the rows' parts alone would take 192 registers)
+  static constexpr int PITCH3 = attn_pitch(DP * 2), PART = 32 * PITCH3;   // a tile of 32 keys as three bf16 parts, keys and values
+  static_assert(!PARTS || 6 * PART <= LDS, "LDS");
   // where chunk c of key `row` lies: at c ^ key. Keys: 16 lanes read one chunk of 16 keys. Values: 16 lanes read 32 bytes of four
   // keys, two such sets side by side (bf16); 32 lanes read 128 bytes of a key and the others of the fourth key on (fp32).
   static __device__ __forceinline__ int k_key(int row) { return CP == 8 ? (row >> 1) & 7 : row & 15; }
@@ -158,24 +167,25 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
   }
 
   // ---- the rows' operands: 16 bytes at 32 ks + 16 half
+  // ---- and what this lane fetches of a tile
   u32x4 fq[KS];
-  const char* const qp = p.q + at_row * p.q_token + qh * p.q_head;
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    const int at = ks * 32 + half * 16;
-    fq[ks] = u32x4{0u, 0u, 0u, 0u};
-    if (live && at < p.head_dim * E) fq[ks] = *(const u32x4*)(qp + at);
-  }
-
-  // ---- what this lane fetches of a tile
   unsigned k_off[LD], v_off[LD];
+  const char* const qp = p.q + at_row * p.q_token + qh * p.q_head;
+  auto get_ready = [&]() __attribute__((always_inline)) {
 #pragma unroll
-  for (int i = 0; i < LD; ++i) {
-    const int at = (wave + 4 * i) * 1024 + lane * 16, r = at / PITCH, c = at % PITCH / 16;
-    const int ck = c ^ S::k_key(r), cv = c ^ S::v_key(r);
-    k_off[i] = ck * 16 < p.head_dim * E ? (unsigned)(r * (int)p.k_token + ck * 16) : kOut;
-    v_off[i] = cv * 16 < p.head_dim * E ? (unsigned)(r * (int)p.v_token + cv * 16) : kOut;
-  }
+    for (int ks = 0; ks < KS; ++ks) {
+      const int at = ks * 32 + half * 16;
+      fq[ks] = u32x4{0u, 0u, 0u, 0u};
+      if (live && at < p.head_dim * E) fq[ks] = *(const u32x4*)(qp + at);
+    }
+#pragma unroll
+    for (int i = 0; i < LD; ++i) {
+      const int at = (wave + 4 * i) * 1024 + lane * 16, r = at / PITCH, c = at % PITCH / 16;
+      const int ck = c ^ S::k_key(r), cv = c ^ S::v_key(r);
+      k_off[i] = ck * 16 < p.head_dim * E ? (unsigned)(r * (int)p.k_token + ck * 16) : kOut;
+      v_off[i] = cv * 16 < p.head_dim * E ? (unsigned)(r * (int)p.v_token + cv * 16) : kOut;
+    }
+  };
   const char* const kp = p.k + (long long)k0 * p.k_token + head * p.k_head;
   const char* const vp = p.v + (long long)k0 * p.v_token + head * p.v_head;
   auto issue = [&](int t, int buf) __attribute__((always_inline)) {   // (keys past the sequence's last arrive as zeros)
@@ -368,15 +378,159 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
       }
     }
   };
-  pass(std::false_type{});
+  // fp32 on the bf16 matrix cores: a value is the sum of three bf16 values, a product of two values the sum of the six largest partial products
+  // (see conv_split.hpp): 192 cycles where the fp32 instructions take 512. Tiles of 32 keys pass through registers, where they are split, a tile ahead, into one
+  // buffer. What is not finite afterwards goes through the fp32 instructions.
+  auto pass_of_parts = [&]() __attribute__((always_inline)) {
+    constexpr int P3 = S::PITCH3, PART = S::PART, CH = DP / 32, K3 = DP / 16;
+    typedef AttnShape<__bf16, DP> B;   // (where chunks of a key lie)
+    const float c3 = c * kSplitUnscale;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    // the rows' parts: 8 values from 16 ks + 8 half on
+    u32x4 q3[K3][3];
+#pragma unroll
+    for (int ks = 0; ks < K3; ++ks) {
+      const int at = ks * 64 + half * 32;
+      u32x4 a = {0u, 0u, 0u, 0u}, b = a;
+      if (live && at < p.head_dim * E) { a = *(const u32x4*)(qp + at); b = *(const u32x4*)(qp + at + 16); }
+      split_bf16(a, b, q3[ks]);
+    }
+    // this thread's part of a tile: four values from 4 (tid mod 8 + 8 i) on of key tid / 8
+    const int r = threadIdx.x >> 3, c8 = threadIdx.x & 7;
+    unsigned kv_off[CH], to_k[CH], to_v[CH];
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int c4 = c8 + 8 * i;
+      kv_off[i] = c4 * 4 < p.head_dim ? (unsigned)(c4 * 16) : kOut;
+      to_k[i] = r * P3 + ((c4 / 2) ^ B::k_key(r)) * 16 + (c4 & 1) * 8;
+      to_v[i] = 3 * PART + r * P3 + ((c4 / 2) ^ B::v_key(r)) * 16 + (c4 & 1) * 8;
+    }
+    u32x4 next[2][CH];
+    auto fetch = [&](int t) __attribute__((always_inline)) {   // (keys past the sequence's last arrive as zeros)
+      const int left = min(nk - t * 32, 32);
+      const bool here = r < left;
+      const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kp + (long long)t * 32 * p.k_token), 0, 0x7fffffff, 0x00020000);
+      const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp + (long long)t * 32 * p.v_token), 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        const bool ok = here && kv_off[i] != kOut;
+        next[0][i] = __builtin_amdgcn_raw_buffer_load_b128(kb, (int)(ok ? r * (unsigned)p.k_token + kv_off[i] : kOut), 0, 0);
+        next[1][i] = __builtin_amdgcn_raw_buffer_load_b128(vb, (int)(ok ? r * (unsigned)p.v_token + kv_off[i] : kOut), 0, 0);
+      }
+    };
+    const int u0 = t0 * (KT / 32), u1 = min(t1 * (KT / 32), (all + 31) / 32);
+    if (u0 < u1) fetch(u0);
+    const unsigned char* const k_from = smem + (lane & 31) * P3;
+    const int k_key = B::k_key(lane & 31), s16 = lane & 15, v_row = 4 * half + s16 / 4;
+    const unsigned char* const v_from = smem + 3 * PART + v_row * P3 + (s16 & 1) * 8;
+    const int v_chunk = (2 * ((lane >> 4) & 1) + (s16 & 3) / 2) ^ B::v_key(v_row);
+    for (int t = u0; t < u1; ++t) {
+      barrier();   // (no wavefront reads the tile before)
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        uint2 part[3];
+        split_bf16(__builtin_bit_cast(f32x4, next[0][i]), part);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) *(uint2*)(smem + e * PART + to_k[i]) = part[e];
+        split_bf16(__builtin_bit_cast(f32x4, next[1][i]), part);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) *(uint2*)(smem + e * PART + to_v[i]) = part[e];
+      }
+      if (t + 1 < u1) fetch(t + 1);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      barrier();
+      const int key0 = t * 32;
+      if (key0 >= most) continue;
+      f32x16 s;
+#pragma unroll
+      for (int ks = 0; ks < K3; ++ks) {
+        u32x4 k3[3];
+#pragma unroll
+        for (int e = 0; e < 3; ++e) k3[e] = *(const u32x4*)(k_from + e * PART + ((2 * ks + half) ^ k_key) * 16);
+#pragma unroll
+        for (int e = 0; e < 6; ++e) {
+          if (ks == 0 && e == 0) s = mma_first<__bf16>(k3[kSplitW[e]], q3[ks][kSplitX[e]]);
+          else mma<__bf16>(k3[kSplitW[e]], q3[ks][kSplitX[e]], s);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      if (key0 + 32 > least) {
+        const int upto = sees - key0 - 4 * half;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = (i / 4) * 8 + i % 4 < upto ? s[i] : -INFINITY;
+      }
+      float top = s[0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[i]);
+      const float now = max_of_halves(top) * c3;
+      if (__any(!(now <= m + kSlack))) {
+        const float grown = __builtin_elementwise_maximum(m, now), by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
+        m = grown;
+        l *= by;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) o[d][i] *= by;
+      }
+      const float from = m == -INFINITY ? 0.f : m;
+      float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c3, -from));
+        part[i & 3] += s[i];
+      }
+      l += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        u32x4 w3[3];
+        split_bf16(__builtin_bit_cast(u32x4, f32x4{s[8 * h], s[8 * h + 1], s[8 * h + 2], s[8 * h + 3]}),
+                   __builtin_bit_cast(u32x4, f32x4{s[8 * h + 4], s[8 * h + 5], s[8 * h + 6], s[8 * h + 7]}), w3);
+#pragma unroll
+        for (int d = 0; d < DT; ++d) {
+          u32x4 v3[3];
+#pragma unroll
+          for (int e = 0; e < 3; ++e) {
+            const unsigned char* const at = v_from + e * PART + h * 16 * P3 + (v_chunk ^ (4 * d)) * 16;
+            const u32x2 a = transposed_read(at), b = transposed_read(at + 8 * P3);
+            v3[e] = u32x4{a[0], a[1], b[0], b[1]};
+          }
+#pragma unroll
+          for (int e = 0; e < 6; ++e) mma<__bf16>(v3[kSplitW[e]], w3[kSplitX[e]], o[d]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] *= kSplitUnscale;
+  };
+  auto any_odd = [&]() __attribute__((always_inline)) {
+    bool odd = false;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) < INFINITY);
+    return __syncthreads_or(odd && live) != 0;
+  };
   // Weights of zero times an infinity or a NaN of a value that the row does not see are NaNs. They are rare, and looked for at the end only: then the
   // keys are gone through again, one by one.
-  bool odd = false;
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) < INFINITY);
-  if (__syncthreads_or(odd && live)) pass(std::true_type{});
+  auto passes = [&]() __attribute__((always_inline)) {
+    get_ready();
+    pass(std::false_type{});
+    if (any_odd()) pass(std::true_type{});
+  };
+  if constexpr (S::PARTS) {
+    pass_of_parts();
+    if (any_odd()) passes();
+  } else {
+    passes();
+  }
   l = sum_of_halves(l);
   if (!live) return;
 
@@ -454,7 +608,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
 // sequence), and parts of the keys: those with which the call is estimated to be done first. A workgroup takes `alone` us a tile of keys where it is alone on
 // its compute unit and `shared` where it is one of two; joining reads and writes the parts' outputs and is a launch. Measured with 1, 2, 4, 8, 16, 32 and 64
 // parts, us: a row of 32 heads (8 of keys) on 8 000 keys 144, 78, 44, 27, 19, 17, 21; 8 such rows on 4 000 keys 81, 52, 35, 34, 38, 46, 65; 256 rows on 4 000 keys 83,
-// 52, 35, 37, 49, 73, 137; a prompt of 1 000 rows 27, 41, 47, 67, ..; in fp32 with 12 heads (4) 138, 84, 74, 76, ...
+// 52, 35, 37, 49, 73, 137; a prompt of 1 000 rows 27, 41, 47, 67, ..; in fp32 with 12 heads (4) 138, 66, 60, 70, ...
 struct Cut { int tile0, tiles, splits; };
 Cut cut(const lop_attention_t* op, lop_rows_t rows) {
   const long long group = op->heads_q / op->heads_k;
@@ -465,7 +619,7 @@ Cut cut(const lop_attention_t* op, lop_rows_t rows) {
   if (op->max_keys < LOP_ATTENTION_CUT) return c;
   struct Price { int keys; double alone, shared; };   // (shared 0: a workgroup has its compute unit for itself)
   static constexpr Price prices[2][4] = {{{64, 0.9, 1.2}, {64, 1.1, 1.7}, {64, 1.3, 2.0}, {64, 2.9, 0.0}},     // bf16: 64, 96, 128, 256 values a head
-                                         {{64, 4.4, 8.0}, {32, 3.0, 5.8}, {32, 4.0, 7.8}, {32, 8.0, 0.0}}};    // fp32
+                                         {{32, 1.7, 3.0}, {32, 2.4, 4.3}, {32, 4.3, 5.9}, {32, 8.9, 0.0}}};    // fp32
   const Price& price = prices[op->dtype == LOP_F32][op->head_dim <= 64 ? 0 : op->head_dim <= 96 ? 1 : op->head_dim <= 128 ? 2 : 3];
   constexpr double kCus = 256.0;
   const double blocks = (double)c.tiles * op->heads_k, band = rows.hi - rows.lo, tiles = (double)ceil_div(op->max_keys, price.keys);
