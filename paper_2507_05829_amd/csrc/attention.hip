@@ -30,7 +30,7 @@ typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr unsigned kOut = 0x80000000u;
 constexpr int kRows = 128;            // of a workgroup: 32 for each of four wavefronts
-constexpr float kSlack = 8.f;
+constexpr float kMostOfTile = 4096.f;
 constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.693147180559945309f;
 
 struct AttnParams {
@@ -95,6 +95,44 @@ __device__ __forceinline__ f32x16 mma_first(const u32x4& a, const u32x4& b) {
     for (int i = 1; i < 4; ++i) s = __builtin_amdgcn_mfma_f32_32x32x2f32(x[i], y[i], s, 0, 0, 0);
     return s;
   }
+}
+
+// Scores become weights 2^(c s - m) of a row, which are added to its sum. What the exponents are relative to, m, need not be the maximum: as long as a tile's
+// weights add up to no more than kMostOfTile nothing overflows and nothing is lost, and it stays. Where they add up to more, as in the first tile, m becomes
+// the maximum so far and output and sum are multiplied. So the maximum is hardly ever formed.
+template <int NB, int DT>
+__device__ __forceinline__ void to_weights(f32x16 (&s)[NB], const float c, float& m, float& l, f32x16 (&o)[DT]) {
+  f32x16 w[NB];
+  auto weights = [&](float from) __attribute__((always_inline)) {
+    float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        w[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -from));
+        part[i & 3] += w[b][i];
+      }
+    return (part[0] + part[1]) + (part[2] + part[3]);
+  };
+  float sum = weights(m);   // (no key so far: m is -infinity, and the sum infinite or a NaN)
+  if (__any(!(sum <= kMostOfTile))) {
+    float top = s[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = b ? 0 : 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[b][i]);
+    const float grown = __builtin_elementwise_maximum(m, max_of_halves(top) * c), by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
+    m = grown;
+    l *= by;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[d][i] *= by;
+    sum = weights(m == -INFINITY ? 0.f : m);
+  }
+  l += sum;
+#pragma unroll
+  for (int b = 0; b < NB; ++b) s[b] = w[b];
 }
 
 constexpr int attn_pitch(int bytes) { return bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
@@ -290,37 +328,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[b][i] = b * 32 + (i / 4) * 8 + i % 4 < upto ? s[b][i] : -INFINITY;
       }
-      // What the exponents are relative to need not be the maximum: it follows where that has grown by more than 2^kSlack, so that sums and
-      // output are hardly ever multiplied.
-      float top[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        top[b] = s[b][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) top[b] = __builtin_elementwise_maximum(top[b], s[b][i]);
-      }
-#pragma unroll
-      for (int b = 1; b < NB; ++b) top[0] = __builtin_elementwise_maximum(top[0], top[b]);
-      const float now = max_of_halves(top[0]) * c;
-      if (__any(!(now <= m + kSlack))) {
-        const float grown = __builtin_elementwise_maximum(m, now), by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
-        m = grown;
-        l *= by;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= by;
-      }
-      const float from = m == -INFINITY ? 0.f : m;   // (no key so far)
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -from));
-          part[i & 3] += s[b][i];
-        }
-      l += (part[0] + part[1]) + (part[2] + part[3]);
+      to_weights(s, c, m, l, o);
       // output
       if constexpr (careful) {
         const int upto = sees - t * KT;
@@ -401,34 +409,27 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
       split_bf16(a, b, q3[ks]);
     }
     // this thread's part of a tile: four values from 4 (tid mod 8 + 8 i) on of key tid / 8
+    // (which lie at their first place ^ 64 i: chunks of 16 bytes, keys of chunks that leave the lowest two bits to 4 i)
     const int r = threadIdx.x >> 3, c8 = threadIdx.x & 7;
-    unsigned kv_off[CH], to_k[CH], to_v[CH];
-#pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int c4 = c8 + 8 * i;
-      kv_off[i] = c4 * 4 < p.head_dim ? (unsigned)(c4 * 16) : kOut;
-      to_k[i] = r * P3 + ((c4 / 2) ^ B::k_key(r)) * 16 + (c4 & 1) * 8;
-      to_v[i] = 3 * PART + r * P3 + ((c4 / 2) ^ B::v_key(r)) * 16 + (c4 & 1) * 8;
-    }
+    const int to_k = r * P3 + ((c8 / 2) ^ B::k_key(r)) * 16 + (c8 & 1) * 8, to_v = 3 * PART + r * P3 + ((c8 / 2) ^ B::v_key(r)) * 16 + (c8 & 1) * 8;
+    const unsigned k_row = r * (unsigned)p.k_token + c8 * 16, v_row = r * (unsigned)p.v_token + c8 * 16;
     u32x4 next[2][CH];
     auto fetch = [&](int t) __attribute__((always_inline)) {   // (keys past the sequence's last arrive as zeros)
-      const int left = min(nk - t * 32, 32);
-      const bool here = r < left;
+      const int columns = t * 32 + r < nk ? p.head_dim - c8 * 4 : 0;
       const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kp + (long long)t * 32 * p.k_token), 0, 0x7fffffff, 0x00020000);
       const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp + (long long)t * 32 * p.v_token), 0, 0x7fffffff, 0x00020000);
 #pragma unroll
       for (int i = 0; i < CH; ++i) {
-        const bool ok = here && kv_off[i] != kOut;
-        next[0][i] = __builtin_amdgcn_raw_buffer_load_b128(kb, (int)(ok ? r * (unsigned)p.k_token + kv_off[i] : kOut), 0, 0);
-        next[1][i] = __builtin_amdgcn_raw_buffer_load_b128(vb, (int)(ok ? r * (unsigned)p.v_token + kv_off[i] : kOut), 0, 0);
+        next[0][i] = __builtin_amdgcn_raw_buffer_load_b128(kb, (int)(i * 32 < columns ? k_row + i * 128 : kOut), 0, 0);
+        next[1][i] = __builtin_amdgcn_raw_buffer_load_b128(vb, (int)(i * 32 < columns ? v_row + i * 128 : kOut), 0, 0);
       }
     };
     const int u0 = t0 * (KT / 32), u1 = min(t1 * (KT / 32), (all + 31) / 32);
     if (u0 < u1) fetch(u0);
     const unsigned char* const k_from = smem + (lane & 31) * P3;
-    const int k_key = B::k_key(lane & 31), s16 = lane & 15, v_row = 4 * half + s16 / 4;
-    const unsigned char* const v_from = smem + 3 * PART + v_row * P3 + (s16 & 1) * 8;
-    const int v_chunk = (2 * ((lane >> 4) & 1) + (s16 & 3) / 2) ^ B::v_key(v_row);
+    const int k_key = B::k_key(lane & 31), s16 = lane & 15, v_key0 = 4 * half + s16 / 4;
+    const unsigned char* const v_from = smem + 3 * PART + v_key0 * P3 + (s16 & 1) * 8;
+    const int v_chunk = (2 * ((lane >> 4) & 1) + (s16 & 3) / 2) ^ B::v_key(v_key0);
     for (int t = u0; t < u1; ++t) {
       barrier();   // (no wavefront reads the tile before)
 #pragma unroll
@@ -436,17 +437,18 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
         uint2 part[3];
         split_bf16(__builtin_bit_cast(f32x4, next[0][i]), part);
 #pragma unroll
-        for (int e = 0; e < 3; ++e) *(uint2*)(smem + e * PART + to_k[i]) = part[e];
+        for (int e = 0; e < 3; ++e) *(uint2*)(smem + e * PART + (to_k ^ (i * 64))) = part[e];
         split_bf16(__builtin_bit_cast(f32x4, next[1][i]), part);
 #pragma unroll
-        for (int e = 0; e < 3; ++e) *(uint2*)(smem + e * PART + to_v[i]) = part[e];
+        for (int e = 0; e < 3; ++e) *(uint2*)(smem + e * PART + (to_v ^ (i * 64))) = part[e];
       }
       if (t + 1 < u1) fetch(t + 1);
       asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
       barrier();
       const int key0 = t * 32;
       if (key0 >= most) continue;
-      f32x16 s;
+      f32x16 tile[1];
+      f32x16& s = tile[0];
 #pragma unroll
       for (int ks = 0; ks < K3; ++ks) {
         u32x4 k3[3];
@@ -464,27 +466,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = (i / 4) * 8 + i % 4 < upto ? s[i] : -INFINITY;
       }
-      float top = s[0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[i]);
-      const float now = max_of_halves(top) * c3;
-      if (__any(!(now <= m + kSlack))) {
-        const float grown = __builtin_elementwise_maximum(m, now), by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
-        m = grown;
-        l *= by;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) o[d][i] *= by;
-      }
-      const float from = m == -INFINITY ? 0.f : m;
-      float part[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c3, -from));
-        part[i & 3] += s[i];
-      }
-      l += (part[0] + part[1]) + (part[2] + part[3]);
+      to_weights(tile, c3, m, l, o);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         u32x4 w3[3];
