@@ -189,11 +189,11 @@ def _load() -> ctypes.CDLL:
                                       POINTER(lop_loss_layer_t), c_double, c_double,
                                       POINTER(lop_two_party_stats_t)]),
         "lop_measure_ceilings": (c_int, [POINTER(lop_ceilings_t)]),
-        "lop_quantize_blocks": (c_int, [c_void_p, lop_rows_t, c_void_p]),
-        "lop_rowwise_f8": (c_int, [c_void_p, lop_rows_t, c_void_p]),
-        "lop_head_norm_rope": (c_int, [c_void_p, lop_rows_t, c_void_p]),
-        "lop_attention_workspace": (c_int, [c_void_p, lop_rows_t, POINTER(c_ulonglong)]),
-        "lop_attention": (c_int, [c_void_p, lop_rows_t, c_void_p]),
+        "lop_quantize_blocks": (c_int, [c_void_p, c_longlong, c_void_p]),
+        "lop_rowwise_f8": (c_int, [c_void_p, c_longlong, c_void_p]),
+        "lop_head_norm_rope": (c_int, [c_void_p, c_longlong, c_void_p]),
+        "lop_attention_workspace": (c_int, [c_void_p, c_longlong, POINTER(c_ulonglong)]),
+        "lop_attention": (c_int, [c_void_p, c_longlong, c_void_p]),
         "lop_debug_guard_check": (c_int, []),
         "lop_strerror": (c_char_p, [c_int]),
         "lop_last_hip_error": (c_int, []),
@@ -418,26 +418,31 @@ def lop_measure_ceilings() -> lop_ceilings_t:
     return c
 
 
+def _rows_word(lo: int, hi: int) -> int:
+    """A lop_rows_t that is passed by value, as the register it travels in (two 32-bit integers, the first in the low half)."""
+    return c_longlong((lo & 0xffffffff) | (hi & 0xffffffff) << 32).value
+
+
 def lop_quantize_blocks(op: lop_quantize_t, rows: Tuple[int, int], stream=None) -> None:
-    _check(_lib.lop_quantize_blocks(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_quantize_blocks")
+    _check(_lib.lop_quantize_blocks(byref(op), _rows_word(*rows), _stream(stream)), "lop_quantize_blocks")
 
 
 def lop_rowwise_f8(op: lop_rowwise_f8_t, rows: Tuple[int, int], stream=None) -> None:
-    _check(_lib.lop_rowwise_f8(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_rowwise_f8")
+    _check(_lib.lop_rowwise_f8(byref(op), _rows_word(*rows), _stream(stream)), "lop_rowwise_f8")
 
 
 def lop_head_norm_rope(op: lop_head_norm_rope_t, rows: Tuple[int, int], stream=None) -> None:
-    _check(_lib.lop_head_norm_rope(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_head_norm_rope")
+    _check(_lib.lop_head_norm_rope(byref(op), _rows_word(*rows), _stream(stream)), "lop_head_norm_rope")
 
 
 def lop_attention_workspace(op: lop_attention_t, rows: Tuple[int, int]) -> int:
     n = c_ulonglong(0)
-    _check(_lib.lop_attention_workspace(byref(op), lop_rows_t(*rows), byref(n)), "lop_attention_workspace")
+    _check(_lib.lop_attention_workspace(byref(op), _rows_word(*rows), byref(n)), "lop_attention_workspace")
     return n.value
 
 
 def lop_attention(op: lop_attention_t, rows: Tuple[int, int], stream=None) -> None:
-    _check(_lib.lop_attention(byref(op), lop_rows_t(*rows), _stream(stream)), "lop_attention")
+    _check(_lib.lop_attention(byref(op), _rows_word(*rows), _stream(stream)), "lop_attention")
 
 
 def lop_debug_guard_check() -> int:
@@ -629,14 +634,14 @@ def _dims(name: str, t, n: int):
     return t.shape
 
 
-def _band(rows, total: int) -> lop_rows_t:
-    return lop_rows_t(0, total) if rows is None else lop_rows_t(*rows)
+_current_device, _current_stream, _grad_enabled = (
+    (torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, torch.is_grad_enabled) if _TYPES else (None, None, None))
 
 
 def _here():
     """The current device, its current stream, whether gradients are recorded."""
-    device = torch.cuda.current_device()
-    return device, torch._C._cuda_getCurrentRawStream(device), torch.is_grad_enabled()
+    device = _current_device()
+    return device, _current_stream(device), _grad_enabled()
 
 
 # Each function first asks in one expression whether everything fits, and goes through the tensors one by one only where
@@ -653,8 +658,8 @@ def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
     (q, scale): q float8_e4m3fn (m, k), scale float32 (ceil(m / block_rows), ceil(k / 128)), allocated with the scales
     of a column of blocks next to one another."""
     device, stream, grad = _here()
-    code, shape = _dtype("x", x), _dims("x", x, 2)
-    m, k = shape
+    code, shape = _TYPES.get(x.dtype) or _dtype("x", x), x.shape
+    m, k = shape if len(shape) == 2 else _dims("x", x, 2)
     if block_rows != 1 and block_rows != LOP_F8_BLOCK:
         _bad("block_rows", f"1 or {LOP_F8_BLOCK}")
     blocks = (-(-m // block_rows), -(-k // LOP_F8_BLOCK))
@@ -668,7 +673,9 @@ def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
             or (grad and (x.requires_grad or q.requires_grad or scale.requires_grad)) or xs[1] != 1 or qs[1] != 1):
         _refuse(device, grad, ("x", x, x.dtype, None, 1), ("q", q, _F8, shape, 1), ("scale", scale, torch.float32, blocks, 0))
     op = _QUANTIZE.pack(m, k, code, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), ss[0], ss[1])
-    _check(_lib.lop_quantize_blocks(op, _band(rows, m), stream), "lop_quantize_blocks")
+    e = _lib.lop_quantize_blocks(op, m << 32 if rows is None else _rows_word(*rows), stream)
+    if e:
+        _check(e, "lop_quantize_blocks")
     return q, scale
 
 
@@ -676,14 +683,16 @@ def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=No
     """act(x W^T + bias + residual) of operands quantized by quantize_blocks: x (m, k) with blocks of one row, w (n, k)
     with blocks of 128 rows (see lop_rowwise_f8). y (m, n) is allocated in `dtype` (None: bfloat16) if it is not passed."""
     device, stream, grad = _here()
-    m, k = _dims("x", x, 2)
-    n, kw = _dims("w", w, 2)
+    x_shape, w_shape = x.shape, w.shape
+    m, k = x_shape if len(x_shape) == 2 else _dims("x", x, 2)
+    n, kw = w_shape if len(w_shape) == 2 else _dims("w", w, 2)
     kb = -(-k // LOP_F8_BLOCK)
     if act not in _ACTS:
         _bad("act", f"one of {sorted(_ACTS)}")
     if y is None:
         y = torch.empty((m, n), dtype=dtype or torch.bfloat16, device=x.device)
-    code, dtype, f32 = _dtype("y", y), y.dtype, torch.float32
+    dtype, f32 = y.dtype, torch.float32
+    code = _TYPES.get(dtype) or _dtype("y", y)
     xs, ws, ys, xss, wss = x.stride(), w.stride(), y.stride(), x_scale.stride(), w_scale.stride()
     if (x.dtype is not _F8 or w.dtype is not _F8 or x_scale.dtype is not f32 or w_scale.dtype is not f32 or kw != k
             or x_scale.shape != (m, kb) or w_scale.shape != (-(-n // LOP_F8_BLOCK), kb) or y.shape != (m, n)
@@ -702,7 +711,9 @@ def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=No
         residual_at, residual_stride = residual.data_ptr(), residual.stride(0)
     op = _ROWWISE_F8.pack(m, n, k, code, _ACTS[act], x.data_ptr(), xs[0], x_scale.data_ptr(), xss[0], xss[1], w.data_ptr(), ws[0],
                           w_scale.data_ptr(), wss[0], wss[1], bias_at, residual_at, residual_stride, y.data_ptr(), ys[0])
-    _check(_lib.lop_rowwise_f8(op, _band(rows, m), stream), "lop_rowwise_f8")
+    e = _lib.lop_rowwise_f8(op, m << 32 if rows is None else _rows_word(*rows), stream)
+    if e:
+        _check(e, "lop_rowwise_f8")
     return y
 
 
@@ -712,8 +723,9 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
     2 * len(freq) values rotated by positions * freq (see lop_head_norm_rope). positions int32 (tokens,), freq float32,
     both None for no rotation. Returns (q_out, k_out), which may be q and k."""
     device, stream, grad = _here()
-    code, dtype, f32, shape = _dtype("q", q), q.dtype, torch.float32, _dims("q", q, 3)
-    tokens, hq, d = shape
+    dtype, f32, shape = q.dtype, torch.float32, q.shape
+    code = _TYPES.get(dtype) or _dtype("q", q)
+    tokens, hq, d = shape if len(shape) == 3 else _dims("q", q, 3)
     if q_out is None:
         q_out = torch.empty(shape, dtype=dtype, device=q.device)
     qs, qos = q.stride(), q_out.stride()
@@ -756,7 +768,9 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
     op = _HEAD_NORM_ROPE.pack(tokens, hq, hk, d, 2 * turns, interleaved, code, eps, amplitude, q.data_ptr(), qs[0], qs[1],
                               k_at, ks[0], ks[1], q_out.data_ptr(), qos[0], qos[1], k_out_at, kos[0], kos[1],
                               q_weight_at, k_weight_at, positions_at, freq_at)
-    _check(_lib.lop_head_norm_rope(op, _band(rows, tokens), stream), "lop_head_norm_rope")
+    e = _lib.lop_head_norm_rope(op, tokens << 32 if rows is None else _rows_word(*rows), stream)
+    if e:
+        _check(e, "lop_head_norm_rope")
     return q_out, k_out
 
 
@@ -767,10 +781,11 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
     sequence as far as known (None: all of k), lse: float32 (heads_q, rows_q) or None, workspace: uint8 of
     lop_attention_workspace bytes (None: allocated). Returns out."""
     device, stream, grad = _here()
-    code, dtype, i32, shape, k_shape = _dtype("q", q), q.dtype, torch.int32, _dims("q", q, 3), _dims("k", k, 3)
-    rows_q, hq, d = shape
-    rows_k, hk, _ = k_shape
-    seqs = _dims("k_begin", k_begin, 1)[0]
+    dtype, i32, shape, k_shape = q.dtype, torch.int32, q.shape, k.shape
+    code = _TYPES.get(dtype) or _dtype("q", q)
+    rows_q, hq, d = shape if len(shape) == 3 else _dims("q", q, 3)
+    rows_k, hk, _ = k_shape if len(k_shape) == 3 else _dims("k", k, 3)
+    seqs = k_begin.shape[0] if k_begin.dim() == 1 else _dims("k_begin", k_begin, 1)[0]
     if out is None:
         out = torch.empty(shape, dtype=dtype, device=q.device)
     qs, ks, vs, os_ = q.stride(), k.stride(), v.stride(), out.stride()
@@ -790,7 +805,7 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
         lse_at = lse.data_ptr()
     if max_keys is None:
         max_keys = rows_k
-    band = _band(rows, rows_q)
+    band = rows_q << 32 if rows is None else _rows_word(*rows)
     fields = (code, hq, hk, d, seqs, rows_q, rows_k, max_keys, causal, scale, q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1],
               v.data_ptr(), vs[0], vs[1], out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), lse_at)
     if workspace is None and max_keys >= LOP_ATTENTION_CUT:
@@ -801,5 +816,7 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
     if workspace is not None:
         _refuse(device, grad, ("workspace", workspace, torch.uint8, (None,), 2))
         workspace_at, workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _check(_lib.lop_attention(_ATTENTION.pack(*fields, workspace_at, workspace_bytes), band, stream), "lop_attention")
+    e = _lib.lop_attention(_ATTENTION.pack(*fields, workspace_at, workspace_bytes), band, stream)
+    if e:
+        _check(e, "lop_attention")
     return out
