@@ -387,8 +387,9 @@ typedef struct {
   void* workspace;          /* device, for the partial results of keys cut into parts; may hold anything  */
   unsigned long long workspace_bytes;
 } lop_attention_t;
-/* Sequences of fewer keys (max_keys) are never cut into parts. */
+/* Sequences of fewer keys (max_keys; in fp32) are never cut into parts. */
 #define LOP_ATTENTION_CUT 512
+#define LOP_ATTENTION_CUT_F32 64
 /* Bytes of workspace that lop_attention wants for these sizes and this band (0: none); the workspace, pointers and device values are not
  * looked at. Given less (or NULL), the call runs without cutting the keys, to the same results up to the order of sums. Calls
  * whose kernels may overlap need a workspace each. */

@@ -598,7 +598,7 @@ Cut cut(const lop_attention_t* op, lop_rows_t rows) {
   c.tile0 = (int)std::max(rows.lo * group / kRows - 1, 0LL);
   c.tiles = (int)((rows.hi * group - 1) / kRows + op->seqs - c.tile0);
   c.splits = 1;
-  if (op->max_keys < LOP_ATTENTION_CUT) return c;
+  if (op->max_keys < (op->dtype == LOP_F32 ? LOP_ATTENTION_CUT_F32 : LOP_ATTENTION_CUT)) return c;
   struct Price { int keys; double alone, shared; };   // (shared 0: a workgroup has its compute unit for itself)
   static constexpr Price prices[2][4] = {{{64, 0.9, 1.2}, {64, 1.1, 1.7}, {64, 1.3, 2.0}, {64, 2.9, 0.0}},     // bf16: 64, 96, 128, 256 values a head
                                          {{32, 1.7, 3.0}, {32, 2.4, 4.3}, {32, 4.3, 5.9}, {32, 8.9, 0.0}}};    // fp32

@@ -103,14 +103,16 @@ __device__ __forceinline__ void put_four(const F8Params& p, f32x4 v, long long m
     for (int i = 0; i < 4; ++i) o[i] = from_f32<T>(clamp_keeping_nan(v[i], cl));
     __builtin_memcpy(__builtin_assume_aligned(y, 4 * sizeof(T)), o, sizeof(o));
   } else {
+    float bias[4] = {0.f, 0.f, 0.f, 0.f}, add[4] = {0.f, 0.f, 0.f, 0.f};   // (first: one wait for all of them)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      if (n + i >= p.n) break;
-      float s = v[i];
-      if (p.bias) s += p.bias[n + i];
-      if (p.res) s += to_f32(r[i]);
-      y[i] = from_f32<T>(clamp_keeping_nan(s, cl));
+      const int at = min(i, p.n - 1 - n);
+      if (p.bias) bias[i] = p.bias[n + at];
+      if (p.res) add[i] = to_f32(r[at]);
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < p.n) y[i] = from_f32<T>(clamp_keeping_nan(v[i] + bias[i] + add[i], cl));
   }
 }
 
@@ -446,22 +448,28 @@ __global__ __launch_bounds__(64 * WM * WN * KG) __attribute__((amdgpu_waves_per_
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-#pragma unroll 4
-        for (int u = 0; u < 16 * TN / 4; ++u) {
-          const int r = u / (TN / 4), c = u % (TN / 4) * 64 + lane;
-          const int row = wm * TM * 16 + i * 16 + r, n = wn * TN * 16 + c;
-          float v = to[r * PITCH + c];
-          const bool ok = row < rows_left && n < n_left;
-          if (p.bias && ok) v += p.bias[n_at + n];
-          if (p.res) {
-            const int at = (int)(ok ? (unsigned)(row * (int)p.res_stride + n * E) : kOut);
-            if constexpr (E == 2) v += to_f32(__builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(rbuf, at, 0, 0)));
-            else v += __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rbuf, at, 0, 0));
+#pragma unroll 1
+        for (int u = 0; u < 2 * (TN / 4); ++u) {   // eight rows of 64 outputs; bias and residual first: one wait for all of them
+          const int c = u / 2 * 64 + lane, n = wn * TN * 16 + c, r0 = u % 2 * 8, row0 = wm * TM * 16 + i * 16 + r0;
+          const bool in = n < n_left;
+          const float bias = p.bias && in ? p.bias[n_at + n] : 0.f;
+          float add[8];
+#pragma unroll
+          for (int r = 0; r < 8; ++r) add[r] = 0.f;
+          if (p.res)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+              const int at = (int)(in && row0 + r < rows_left ? (unsigned)((row0 + r) * (int)p.res_stride + n * E) : kOut);
+              if constexpr (E == 2) add[r] = to_f32(__builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b16(rbuf, at, 0, 0)));
+              else add[r] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(rbuf, at, 0, 0));
+            }
+#pragma unroll
+          for (int r = 0; r < 8; ++r) {
+            const T o = from_f32<T>(clamp_keeping_nan(to[(r0 + r) * PITCH + c] + bias + add[r], cl));
+            const int at = (int)(in && row0 + r < rows_left ? (unsigned)((row0 + r) * (int)p.y_stride + n * E) : kOut);
+            if constexpr (E == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, o), ybuf, at, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o), ybuf, at, 0, 0);
           }
-          const T o = from_f32<T>(clamp_keeping_nan(v, cl));
-          const int at = (int)(ok ? (unsigned)(row * (int)p.y_stride + n * E) : kOut);
-          if constexpr (E == 2) __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(unsigned short, o), ybuf, at, 0, 0);
-          else __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, o), ybuf, at, 0, 0);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();

@@ -41,7 +41,7 @@ LOP_FLAG_NO_FUSE = 32
 LOP_FLAG_POISON_SCRATCH = 64
 LOP_FLAG_BATCH_BANDS = 128
 LOP_LINK_INDEPENDENT, LOP_LINK_QUEUED = 0, 1
-LOP_F8_BLOCK, LOP_ATTENTION_CUT = 128, 512
+LOP_F8_BLOCK, LOP_ATTENTION_CUT, LOP_ATTENTION_CUT_F32 = 128, 512, 64
 
 
 def LOP_FLAG_LANES(n: int) -> int:
@@ -808,7 +808,7 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
     band = rows_q << 32 if rows is None else _rows_word(*rows)
     fields = (code, hq, hk, d, seqs, rows_q, rows_k, max_keys, causal, scale, q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1],
               v.data_ptr(), vs[0], vs[1], out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), lse_at)
-    if workspace is None and max_keys >= LOP_ATTENTION_CUT:
+    if workspace is None and max_keys >= (LOP_ATTENTION_CUT_F32 if code == LOP_F32 else LOP_ATTENTION_CUT):
         n = c_ulonglong(0)
         _check(_lib.lop_attention_workspace(_ATTENTION.pack(*fields, 0, 0), band, byref(n)), "lop_attention_workspace")
         if n.value:
