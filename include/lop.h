@@ -360,8 +360,8 @@ LOP_API int lop_head_norm_rope(const lop_head_norm_rope_t* op, lop_rows_t rows, 
  * that sees none is zeros, its lse -infinity. Rows of q before the first or behind the last sequence, and their out and lse, are left as they are. Keys and values
  * that a row does not see do not touch it, whatever they hold. A local operator in its rows once a sequence's keys are
  * there: a band needs no other row of q.
- * Scores, maxima, sums and outputs are held in fp32; with bf16 storage the weights exp(score - maximum) are rounded to bf16 for their product with
- * v (their sum is taken of the unrounded ones).
+ * Scores, sums and outputs are held in fp32; with bf16 storage the weights are rounded to bf16 for their product with v (their sum is taken of the
+ * unrounded ones), fp32 products of heads up to 128 values are sums of six products of bf16 parts (off by 2^-24 of a product at most).
  * The offsets are read on the device; what lies outside 0 .. rows_q or rows_k is cut off there. */
 typedef struct {
   int dtype;                /* LOP_F32 or LOP_BF16                                                        */
