@@ -6,8 +6,11 @@
 // A lane holds two groups of four consecutive values that need no other lane's: of neighbouring pairs two groups side by side, of
 // pairs half the rotated part apart the same place in both halves; what is not rotated follows eight by eight. A head is 8, 16 or 32 lanes, and the
 // cosines of a lane's four pairs serve every head of its token that the wavefront goes through: they cost as much as several
-// heads, since far positions need their angle reduced in 64 bits. Bound by memory.
+// heads, since far positions need their angle reduced in 64 bits. Bound by memory: 16384 tokens of 40 heads of 128 values take 68 us in bf16
+// (4.9 TB/s), 118 us in fp32 (5.7 TB/s); one token 3 us, which a launch in a graph and three loads one after the other take.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "launch.hpp"
 #include "lop.h"
@@ -151,13 +154,17 @@ int rope(const lop_head_norm_rope_t* op, lop_rows_t rows, hipStream_t stream) {
   p.heads_q = op->heads_q; p.heads_k = op->heads_k; p.head_dim = op->head_dim; p.rot_dim = op->rot_dim; p.interleaved = op->interleaved != 0;
   p.eps = op->eps; p.amplitude = op->amplitude; p.by_dim = 1.f / (float)op->head_dim;
   const int lanes = op->head_dim <= 64 ? 8 : op->head_dim <= 128 ? 16 : 32;
-  // A wavefront takes all heads of its token, unless that leaves it with few tokens: then each round of heads has a wavefront.
+  // A round: the heads that lie side by side in a wavefront. Several rounds to a wavefront share its cosines, but take as long as they do: as many as leave
+  // 4096 wavefronts, of fp32, whose rounds outlast the cosines of another wavefront, two at most. Measured, us, 40 heads of 128 values (ten rounds), bf16: 64
+  // tokens 3.5 with one round and 10.8 with all, 1024 tokens 8.4 with two, 10.0 with one, 15.6 with all, 4096 tokens 21.5 with all, 29 with one, 16384 tokens
+  // 68 and 107; of fp32 4096 tokens 34 with two, 35 with one, 39 with all, 16384 tokens 118, 124 and 132.
   const long long tokens = rows.hi - rows.lo;
   const int heads = op->heads_q + op->heads_k, side = 64 / lanes, rounds = (heads + side - 1) / side;
-  const int parts = tokens >= 4096 ? 1 : rounds;
-  p.per_part = (rounds + parts - 1) / parts * side;
-  p.parts = parts;
-  const long long grid = ceil_div(tokens * parts, 4);
+  const int most = E == 4 ? 2 : rounds;
+  const int each = (int)std::min<long long>(most, std::max<long long>(1, rounds * tokens / 4096));   // rounds of heads of a wavefront
+  p.per_part = each * side;
+  p.parts = (rounds + each - 1) / each;
+  const long long grid = ceil_div(tokens * p.parts, 4);
   if (grid > launch_blocks(256)) return LOP_ERR_UNSUPPORTED;
   const dim3 g((unsigned)grid), b(256);
   LOP_HIP(lanes == 8    ? launch_kernel(head_norm_rope_kernel<T, 8>, g, b, stream, nullptr, p)
