@@ -460,3 +460,97 @@ def test_operators_refuse_what_does_not_fit():
         with pytest.raises(lop.LopError) as err:
             bad()
         assert err.value.code == code
+
+
+# ------------------------------------------------------------------ calls that share something
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("tokens,hq,hk,d", [(700, 20, 6, 128), (1300, 20, 6, 128), (4200, 20, 6, 128), (2000, 9, 0, 256), (3000, 40, 3, 64)])
+def test_head_norm_rope_several_heads_in_turn(tokens, hq, hk, d, dtype):
+    """Wavefronts that go through some of a token's heads, or all, the last of them fewer."""
+    rng = np.random.default_rng(tokens + hq)
+    qk = values(rng, (tokens, hq + hk, d), dtype)
+    pos = rng.integers(0, 1 << 17, tokens).astype(np.int32)
+    freq = (1e6 ** (-2.0 * np.arange(d // 2) / d)).astype(np.float32)
+    w = (1 + 0.1 * rng.standard_normal(d)).astype(np.float32)
+    x = dev(qk, dtype)
+    q_out, k_out = lop.head_norm_rope(x[:, :hq], x[:, hq:] if hk else None, dev(pos), dev(freq), dev(w), dev(w) if hk else None, 1e-6)
+    want, size = plain.norm_rope(qk, pos, freq, w, 1e-6, False, 1.0)
+    got = host(q_out if k_out is None else torch.cat((q_out, k_out), 1))
+    assert_near(got, want, rope_tolerance(want, size, d, dtype), f"{tokens} tokens")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_keys", [None, 10])
+def test_attention_sequences_that_share_keys(dtype, max_keys):
+    """The same keys for several sequences, whole, in part or overlapping, and one without any."""
+    rng = np.random.default_rng(21)
+    q, k, v, *_ = packed(rng, [(9, 900)], 6, 2, 72, dtype)
+    offsets, begin, end = [0, 1, 4, 5, 8, 9], [0, 0, 130, 0, 700], [900, 900, 830, 0, 900]
+    check_attention(attend(q, k, v, offsets, begin, end, dtype, max_keys=max_keys), q, k, v, offsets, begin, end, dtype)
+
+
+def test_calls_at_once_on_two_streams():
+    """Each with its own workspace and outputs: what one call at a time gives, bit for bit."""
+    rng = np.random.default_rng(22)
+    jobs = []
+    for dtype, d in (("bf16", 128), ("f32", 64)):
+        q, k, v, offsets, begin, end = packed(rng, [(1, 3000), (2, 1700)], 8, 2, d, dtype)
+        args = [dev(a, dtype) for a in (q, k, v)] + [dev(np.array(a, np.int32)) for a in (offsets, begin, end)]
+        jobs.append(lambda args=args, d=d: lop.attention(*args, d ** -0.5))
+    for m in (1, 40, 600):
+        x, w = lop.quantize_blocks(dev(values(rng, (m, 1040), "f32"))), lop.quantize_blocks(dev(values(rng, (400, 1040), "f32")), 128)
+        jobs.append(lambda x=x, w=w: lop.rowwise_f8(*x, *w))
+    alone = [job() for job in jobs]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+    for i in range(12):
+        for j, job in enumerate(jobs):
+            with torch.cuda.stream(streams[(i + j) % 2]):
+                got.append((j, job()))
+    torch.cuda.synchronize()
+    for j, y in got:
+        assert torch.equal(y, alone[j])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_cache_that_grows_between_replays(dtype):
+    """One captured step whose keys are cut into parts; its offsets, inputs and cache change between the replays, the graph does not."""
+    rng = np.random.default_rng(23)
+    room, hq, hk, d = 2100, 8, 2, 64
+    k, v = (values(rng, (2 * room, hk, d), dtype) for _ in range(2))
+    k_dev, v_dev = dev(k, dtype), dev(v, dtype)
+    q_dev = torch.zeros(2, hq, d, dtype=TORCH[dtype], device="cuda")
+    ofs, begin = dev(np.array([0, 1, 2], np.int32)), dev(np.array([0, room], np.int32))
+    end = dev(np.array([1, room], np.int32))
+    out = torch.empty_like(q_dev)
+    lse = torch.empty(hq, 2, device="cuda")
+
+    def step():
+        lop.attention(q_dev, k_dev, v_dev, ofs, begin, end, d ** -0.5, max_keys=room, out=out, lse=lse)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            step()
+    torch.cuda.synchronize()
+    for lens in ((1, 0), (0, 2100), (700, 31), (2100, 2100), (64, 65)):
+        q = values(rng, (2, hq, d), dtype)
+        q_dev.copy_(dev(q, dtype))
+        end.copy_(dev(np.array([lens[0], room + lens[1]], np.int32)))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        got, got_lse = out.clone(), lse.clone()
+        ends = [lens[0], room + lens[1]]
+        check_attention((host(got), host(got_lse)), q, k, v, [0, 1, 2], [0, room], ends, dtype)
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got) and torch.equal(lse, got_lse)
