@@ -7,6 +7,9 @@
 // rounding to bf16 by a factor of 100. For fp32 outputs that would show: there the operands, which bf16 holds exactly, go through the bf16 instructions at
 // half the rate, whose sums are off by 1e-7.) The weights are the instruction's rows and the matrix rows its columns, so that a lane's results
 // share a matrix row, one product of two scales does for all of them, and they lie next to one another in y.
+//
+// Bound: large products by the matrix instructions and the scaling between them: 16384 x 4096 to 16384 outputs take 1013 us, 2.17 PFLOP/s (a library
+// product without scales 2.6); few rows by reading the weights: 48 rows of 4096 to 4096 9.8 us, where the launch and the way to memory are most of it.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -574,17 +577,17 @@ __global__ __launch_bounds__(64 * NW) void rowwise_f8_few_kernel(const F8Params 
   }
 }
 
-// Which kernel: the one that is estimated to be done first. Time of a launch = start + rounds * (each + blocks of columns * step), where a round is a
-// workgroup (128 x 128: two) on every compute unit. Measured,
-// us, bf16 and fp32 outputs, 4096 columns (32 blocks): 16 x 32 outputs 5.5 a round, 32 x 32 8.2, 32 x 64 10.5; 64 x 128 (two groups) 17.5 and
-// 26, 128 x 128 38 and 72 (25 and 42 where one is on a unit), 256 x 256 63. So 48 rows to 4096 columns take 9.8 (32 x 32; 12.9 with 16 x 32, 13.9 with 32 x 64),
-// 96 rows 14.0 (32 x 64; 18.1 with 64 x 128, 24.5 with 128 x 128), 512 rows 20.0 (25.4 with 128 x 128, 45.7 with 32 x 64), 2048 rows 42 (58.8 with 256 x 256, 87.6 with 64 x 128) and
-// 4096 rows 69 (80 with 128 x 128).
+// Which kernel: the one that is estimated to be done first. Time of a launch, us = start + rounds * (each + blocks of columns * step), where a round is a
+// workgroup (128 x 128: two) on every compute unit. Fitted to 217 products of 1 to 16384 rows, 256 to 8192 columns and 128 to 16384 outputs that were timed
+// with every kernel: the chosen one is the fastest to 0.2 % in the mean, to 7 % at worst. Measured, us, bf16, 4096 columns: 48 rows to 4096 outputs 9.8 (32 x 32;
+// 12.9 with 16 x 32, 13.9 with 32 x 64), 96 rows 14.0 (32 x 64; 18.1 with 64 x 128, 24.5 with 128 x 128), 512 rows 20.0 (64 x 128; 25.4 with 128 x 128, 45.7 with
+// 32 x 64), 2048 rows 42 (128 x 128; 58.8 with 256 x 256, 87.6 with 64 x 128) and 4096 rows 69 (256 x 256; 80 with 128 x 128). Of few columns the stores are
+// most of it: 256 columns, 10228 rows to 2983 outputs take 40 with 128 x 128, 47 with 256 x 256, 110 with 32 x 64, 135 with 64 x 128.
 constexpr int kCus = 256;
 int choose(long long m, long long n, int k, bool f32) {
   struct Shape { int bm, bn; double start, each, step, step_f32; };
-  static constexpr Shape shapes[] = {{16, 32, 1.0, 0.0, 0.17, 0.17}, {32, 32, 1.5, 0.0, 0.25, 0.25}, {32, 64, 3.0, 0.0, 0.33, 0.33},
-                                     {64, 128, 2.0, 0.0, 0.54, 0.80}, {128, 128, 3.0, 2.0, 1.15, 2.2}, {256, 256, 8.0, 5.0, 1.8, 0.0}};
+  static constexpr Shape shapes[] = {{16, 32, 1.1, 0.4, 0.15, 0.17}, {32, 32, 0.3, 0.9, 0.28, 0.30}, {32, 64, 2.1, 0.4, 0.35, 0.36},
+                                     {64, 128, 2.4, 3.1, 0.50, 0.96}, {128, 128, 3.6, 2.7, 1.32, 2.13}, {256, 256, 8.0, 5.2, 1.8, 0.0}};
   const double blocks = (double)ceil_div(k, kBlock);
   int best = 0;
   double least = 0.0;
