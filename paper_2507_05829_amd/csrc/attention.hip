@@ -595,7 +595,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
 // its compute unit and `shared` where it is one of two; joining reads and writes the parts' outputs and is a launch. Measured with 1, 2, 4, 8, 16, 32 and 64
 // parts, us: a row of 32 heads (8 of keys) on 8 000 keys 144, 78, 44, 27, 19, 17, 21; 8 such rows on 4 000 keys 81, 52, 35, 34, 38, 46, 65; 256 rows on 4 000 keys 83,
 // 52, 35, 37, 49, 73, 137; a prompt of 1 000 rows 27, 41, 47, 67, ..; in fp32 with 12 heads (4) 138, 66, 60, 70, ...
-// Of 60 calls of all kinds the chosen number is within 3 % of the best in the mean, and 34 % off at worst (caches filled to a half on the average).
+// Of 120 calls of all kinds the chosen number is within 3 % of the best in the mean, and 34 % off at worst (caches filled to a half on the average).
 struct Cut { int tile0, tiles, splits; };
 Cut cut(const lop_attention_t* op, lop_rows_t rows) {
   const long long group = op->heads_q / op->heads_k;
