@@ -360,7 +360,7 @@ LOP_API int lop_head_norm_rope(const lop_head_norm_rope_t* op, lop_rows_t rows, 
  * that sees none is zeros, its lse -infinity. Rows of q before the first or behind the last sequence, and their out and lse, are left as they are. Keys and values
  * that a row does not see do not touch it, whatever they hold. A local operator in its rows once a sequence's keys are
  * there: a band needs no other row of q.
- * Scores, sums and outputs are held in fp32; with bf16 storage the weights are rounded to bf16 for their product with v (their sum is taken of the
+ * Scores, sums and outputs are held in fp32 (a row may be NaN where a score, or that times scale / ln 2, passes its range); with bf16 storage the weights are rounded to bf16 for their product with v (their sum is taken of the
  * unrounded ones), fp32 products of heads up to 128 values are sums of six products of bf16 parts (off by 2^-24 of a product at most).
  * Rows of k and of v do not overlap (k_token and v_token at least head_dim) and are at most 16 MiB apart.
  * The offsets are read on the device; what lies outside 0 .. rows_q or rows_k is cut off there. */

@@ -139,6 +139,32 @@ __device__ __forceinline__ void to_weights(f32x16 (&s)[NB], const float c, float
   for (int b = 0; b < NB; ++b) s[b] = w[b];
 }
 
+// The same for the careful pass: m is the maximum of the unscaled scores so far, followed at every step, and weights are 2^(c (s - m)). Of scores from 2^31 on c s - m
+// is off by a step of m, more than the exponential function's range, where c (s - m) of the maximum is 0.
+template <int NB, int DT>
+__device__ __forceinline__ void to_weights_of_differences(f32x16 (&s)[NB], const float c, float& m, float& l, f32x16 (&o)[DT]) {
+  float top = m;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[b][i]);
+  top = max_of_halves(top);
+  const float by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c), from = top == -INFINITY ? 0.f : top;
+  m = top;
+  l *= by;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] *= by;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[b][i] = __builtin_amdgcn_exp2f((s[b][i] - from) * c);
+      l += s[b][i];
+    }
+}
+
 constexpr int attn_pitch(int bytes) { return bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
 
 // DP: head_dim rounded up to what is computed (a multiple of 32)
@@ -332,7 +358,8 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[b][i] = b * 32 + (i / 4) * 8 + i % 4 < upto ? s[b][i] : -INFINITY;
       }
-      to_weights(s, c, m, l, o);
+      if constexpr (careful) to_weights_of_differences(s, c, m, l, o);
+      else to_weights(s, c, m, l, o);
       // output
       if constexpr (careful) {
         const int upto = sees - t * KT;
@@ -389,10 +416,13 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
         });
       }
     }
+    if constexpr (careful) m *= c;
   };
   // fp32 on the bf16 matrix cores: a value is the sum of three bf16 values, a product of two values the sum of the six largest partial products
   // (see conv_split.hpp): 192 cycles where the fp32 instructions take 512. Tiles of 32 keys pass through registers, where they are split, a tile ahead, into one
-  // buffer. What is not finite afterwards goes through the fp32 instructions.
+  // buffer. Scores are 2^48 times as large as they are, so that some are infinite here and finite in fp32: rows of such a score, which a weight of zero
+  // would hide, and of an output that is not finite go through the fp32 instructions afterwards.
+  float low = 0.f;   // the least score that the row sees, where it is negative
   auto pass_of_parts = [&]() __attribute__((always_inline)) {
     constexpr int P3 = S::PITCH3, PART = S::PART, CH = DP / 32, K3 = DP / 16;
     typedef AttnShape<__bf16, DP> B;   // (where chunks of a key lie)
@@ -468,7 +498,14 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
       if (key0 + 32 > least) {
         const int upto = sees - key0 - 4 * half;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = (i / 4) * 8 + i % 4 < upto ? s[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const bool seen = (i / 4) * 8 + i % 4 < upto;
+          low = __builtin_elementwise_minimum(low, seen ? s[i] : 0.f);
+          s[i] = seen ? s[i] : -INFINITY;
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) low = __builtin_elementwise_minimum(low, s[i]);
       }
       to_weights(tile, c3, m, l, o);
 #pragma unroll
@@ -496,8 +533,12 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] *= kSplitUnscale;
   };
+  // Also looked at: the sum of the weights. Relative to a score far from zero (see to_weights_of_differences) all may vanish; else the largest is 2^-12 at
+  // least, and with the least sum here no other weight of more than 2^-62 of it is lost.
+  constexpr float kLeastSum = 0x1p-64f;
   auto any_odd = [&]() __attribute__((always_inline)) {
-    bool odd = false;
+    const float sum = sum_of_halves(l);
+    bool odd = !(low > -INFINITY) || (sees > t0 * KT && !(sum >= kLeastSum));
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -508,6 +549,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
   // keys are gone through again, one by one.
   auto passes = [&]() __attribute__((always_inline)) {
     get_ready();
+    low = 0.f;
     pass(std::false_type{});
     if (any_odd()) pass(std::true_type{});
   };
