@@ -43,7 +43,7 @@ struct AttnParams {
   long long q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;   // bytes
   const int *q_offsets, *k_begin, *k_end;
   float* lse;
-  float* part;       // of keys cut into parts: [split][row of the band][head][head_dim] of the output, then [..][2] of maximum and sum
+  float* part;       // of keys cut into parts: [split][row of the band][head][head_dim] of the part's mean, then [..][2] of maximum and sum
   int heads_k, group, head_dim, seqs, rows_q, rows_k, causal;
   int lo, hi;        // the band
   int tile0, tiles;  // of packed rows
@@ -140,29 +140,36 @@ __device__ __forceinline__ void to_weights(f32x16 (&s)[NB], const float c, float
 }
 
 // The same for the careful pass: m is the maximum of the unscaled scores so far, followed at every step, and weights are 2^(c (s - m)). Of scores from 2^31 on c s - m
-// is off by a step of m, more than the exponential function's range, where c (s - m) of the maximum is 0.
+// is off by a step of m, more than the exponential function's range, where c (s - m) of the maximum is 0. The output is the weighted mean so far and the weights
+// are shares of their sum, l, which both lanes of a row have here: values that fp32 holds have a mean that it holds, while their sums may pass its range.
 template <int NB, int DT>
-__device__ __forceinline__ void to_weights_of_differences(f32x16 (&s)[NB], const float c, float& m, float& l, f32x16 (&o)[DT]) {
+__device__ __forceinline__ void to_shares(f32x16 (&s)[NB], const float c, float& m, float& l, f32x16 (&o)[DT]) {
   float top = m;
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[b][i]);
   top = max_of_halves(top);
-  const float by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - top) * c), from = top == -INFINITY ? 0.f : top;
-  m = top;
-  l *= by;
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) o[d][i] *= by;
+  const float before = m == -INFINITY ? 0.f : l * __builtin_amdgcn_exp2f((m - top) * c), from = top == -INFINITY ? 0.f : top;
+  float sum = 0.f;
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       s[b][i] = __builtin_amdgcn_exp2f((s[b][i] - from) * c);
-      l += s[b][i];
+      sum += s[b][i];
     }
+  m = top;
+  l = before + sum_of_halves(sum);
+  const float by = l == 0.f ? 0.f : 1.f / l, keep = before * by;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) o[d][i] *= keep;
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) s[b][i] *= by;
 }
 
 constexpr int attn_pitch(int bytes) { return bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
@@ -291,6 +298,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 
   const float c = p.scale * kLog2e;
   f32x16 o[DT];
+  bool shares = false;   // the output is the mean already
   float m, l;   // what the exponents of c s are relative to, in powers of two; sum
   auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
@@ -358,7 +366,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[b][i] = b * 32 + (i / 4) * 8 + i % 4 < upto ? s[b][i] : -INFINITY;
       }
-      if constexpr (careful) to_weights_of_differences(s, c, m, l, o);
+      if constexpr (careful) to_shares(s, c, m, l, o);
       else to_weights(s, c, m, l, o);
       // output
       if constexpr (careful) {
@@ -367,7 +375,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
         for (int b = 0; b < NB; ++b)
 #pragma unroll 1
           for (int i = 0; i < 16; ++i) {
-            const float mine = (float)(T)s[b][i], other = __shfl_xor(mine, 32, 64);
+            const float mine = s[b][i], other = __shfl_xor(mine, 32, 64);
 #pragma unroll 1
             for (int h = 0; h < 2; ++h) {
               const int key = b * 32 + (i / 4) * 8 + h * 4 + i % 4;
@@ -416,7 +424,10 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
         });
       }
     }
-    if constexpr (careful) m *= c;
+    if constexpr (careful) {
+      m *= c;
+      shares = true;
+    }
   };
   // fp32 on the bf16 matrix cores: a value is the sum of three bf16 values, a product of two values the sum of the six largest partial products
   // (see conv_split.hpp): 192 cycles where the fp32 instructions take 512. Tiles of 32 keys pass through registers, where they are split, a tile ahead, into one
@@ -533,7 +544,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] *= kSplitUnscale;
   };
-  // Also looked at: the sum of the weights. Relative to a score far from zero (see to_weights_of_differences) all may vanish; else the largest is 2^-12 at
+  // Also looked at: the sum of the weights. Relative to a score far from zero (see to_shares) all may vanish; else the largest is 2^-12 at
   // least, and with the least sum here no other weight of more than 2^-62 of it is lost.
   constexpr float kLeastSum = 0x1p-64f;
   auto any_odd = [&]() __attribute__((always_inline)) {
@@ -559,8 +570,9 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
   } else {
     passes();
   }
-  l = sum_of_halves(l);
+  if (!shares) l = sum_of_halves(l);
   if (!live) return;
+  const float by = shares ? 1.f : l == 0.f ? 0.f : 1.f / l;   // (no key: a row that sees none, or none of this part)
 
   if (p.splits > 1) {
     const long long rows = (long long)(p.hi - p.lo) * (p.heads_k * p.group);
@@ -571,12 +583,12 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int at = d * 32 + j * 8 + half * 4;
-        if (at < p.head_dim) *(f32x4*)(to + at) = f32x4{o[d][j * 4], o[d][j * 4 + 1], o[d][j * 4 + 2], o[d][j * 4 + 3]};
+        if (at < p.head_dim) *(f32x4*)(to + at) = f32x4{o[d][j * 4] * by, o[d][j * 4 + 1] * by, o[d][j * 4 + 2] * by, o[d][j * 4 + 3] * by};
       }
     if (half == 0) *(float2*)(p.part + p.splits * rows * p.head_dim + slot * 2) = make_float2(m, sees > 0 ? l : -1.f);
     return;
   }
-  const float by = sees > 0 ? 1.f / l : 0.f;
+  const float by_all = l == 0.f ? NAN : by;   // (no seen score is one that fp32 holds)
   char* const op = p.out + at_row * p.out_token + qh * p.out_head;
 #pragma unroll
   for (int d = 0; d < DT; ++d)
@@ -586,7 +598,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
       if (at >= p.head_dim) continue;
       alignas(16) T w[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(sees > 0 ? o[d][j * 4 + e] * by : 0.f);
+      for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(sees > 0 ? o[d][j * 4 + e] * by_all : 0.f);
       __builtin_memcpy(__builtin_assume_aligned(op + at * E, 4 * E), w, sizeof(w));
     }
   if (p.lse && half == 0) p.lse[(long long)qh * p.rows_q + at_row] = sees > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
@@ -612,6 +624,7 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
   float l = by * mine.y;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) l += __shfl_xor(l, d, 64);
+  const float share = by * mine.y / l;
   const bool here = lane * 4 < p.head_dim;
   const float* const from = p.part + at * p.head_dim + (here ? lane * 4 : 0);
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -621,12 +634,12 @@ __global__ __launch_bounds__(256) void attention_join_kernel(const AttnParams p)
     for (int i = 0; i < 8; ++i) x[i] = *(const f32x4*)(from + min(s0 + i, p.splits - 1) * rows * p.head_dim);
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (s0 + i < p.splits) o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(by), s0 + i)) * x[i];
+      if (s0 + i < p.splits) o += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(share), s0 + i)) * x[i];
   }
   if (here) {
     alignas(16) T w[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = from_f32<T>(none ? 0.f : o[i] / l);
+    for (int i = 0; i < 4; ++i) w[i] = from_f32<T>(none ? 0.f : o[i]);
     __builtin_memcpy(__builtin_assume_aligned(p.out + row * p.out_token + head * p.out_head + lane * 4 * (int)sizeof(T), 4 * sizeof(T)), w, sizeof(w));
   }
   if (p.lse && lane == 0) p.lse[(long long)head * p.rows_q + row] = none ? -INFINITY : (m + log2f(l)) * kLn2;

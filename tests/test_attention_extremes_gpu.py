@@ -88,3 +88,39 @@ def test_far_scores_of_a_small_scale(scale):
     # scores are exact (sums of up to 64 times a whole number below 2^7 times a power of two); scaled and by the logarithm of 2: 2 roundings each,
     # in the difference of two of up to `spread`: relative in the weights
     near(out, want, d, "f32", n, size * (1 + 8 * U32 * spread[..., None] / (2 * n * 2 * U32)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_keys", [1, 5000])
+@pytest.mark.parametrize("size", [2.0 ** 110, 2.0 ** 116, 2.0 ** 127])
+def test_values_near_the_end_of_the_range(size, max_keys, dtype):
+    """Scores that grow a little from key to key, so that the weights relative to those of the first keys are large, and values whose weighted mean is
+    finite while their sums are not."""
+    rng = np.random.default_rng(5)
+    n, d = 600, 64
+    q = np.zeros((3, 2, d), np.float32)
+    q[..., 0] = 1.0
+    k = np.zeros((n, 1, d), np.float32)
+    k[:, 0, 0] = np.floor(np.arange(n) / 64.0) * 2.0
+    v = (values(rng, (n, 1, d), dtype).clip(0.25, 1.0) * np.float32(size)).astype(np.float32)
+    out, _ = attend(q, k, v, [0, 1, 3], [0, 0], [n, 200], dtype, scale=1.0, max_keys=max_keys)
+    want, _, mean, spread = plain.attention(q, k, v, [0, 1, 3], [0, 0], [n, 200], 1.0, True)
+    near(out, want, d, dtype, n, mean * (1 + 8 * U32 * spread[..., None] / (2 * n * 2 * U32)))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_keys", [1, 5000])
+@pytest.mark.parametrize("sign", [-1.0, 1.0])
+def test_scores_past_the_range_show(sign, max_keys, dtype):
+    """Rows of which every score is +-6.4e40 are NaN; where one key's score is 0 and the others' -6.4e40, its value is the result."""
+    rng = np.random.default_rng(6)
+    n, d = 200, 64
+    q, k = np.full((2, 1, d), 2.0 ** 66, np.float32), np.full((2 * n, 1, d), sign * 2.0 ** 63, np.float32)
+    k[n + 50] = 0.0
+    v = values(rng, (2 * n, 1, d), dtype)
+    out, _ = attend(q, k, v, [0, 1, 2], [0, n], [n, 2 * n], dtype, scale=0.125, max_keys=max_keys)
+    assert np.isnan(out[0]).all()
+    if sign > 0:
+        assert np.isnan(out[1]).all()
+    else:
+        near(out[1], v[n + 50].astype(np.float64), d, dtype, 1)
