@@ -358,8 +358,9 @@ LOP_API int lop_head_norm_rope(const lop_head_norm_rope_t* op, lop_rows_t rows, 
  * part begins and how far it is filled). heads_q / heads_k query heads in a row share a key head. out = softmax(scale q k^T) v over the keys a
  * row sees: all of its sequence, or (causal) the first nk - nq + r + 1 for row r of nq: the last row sees every key. A row
  * that sees none is zeros, its lse -infinity. Rows of q before the first or behind the last sequence, and their out and lse, are left as they are. Keys and values
- * that a row does not see do not touch it, whatever they hold. A local operator in its rows once a sequence's keys are
- * there: a band needs no other row of q.
+ * that a row does not see do not touch it, whatever they hold (infinities and NaNs among them may change the order of its sums). A local operator in its rows once a sequence's keys are
+ * there: a band needs no other row of q, and a row's bits are the same in every band and beside any other rows, as long as its keys are cut into the same parts. (The number of parts
+ * depends on the band, the sizes and max_keys; without a workspace it is one.)
  * Scores, sums and outputs are held in fp32 (a row may be NaN where a score, or that times scale / ln 2, passes its range); with bf16 storage the weights are rounded to bf16 for their product with v (their sum is taken of the
  * unrounded ones), fp32 products of heads up to 128 values are sums of six products of bf16 parts (off by 2^-24 of a product at most).
  * Rows of k and of v do not overlap (k_token and v_token at least head_dim) and are at most 16 MiB apart.

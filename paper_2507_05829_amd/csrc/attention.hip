@@ -86,6 +86,11 @@ __device__ __forceinline__ float sum_of_halves(float v) {
   return __uint_as_float((unsigned)s[0]) + __uint_as_float((unsigned)s[1]);
 }
 
+__device__ __forceinline__ bool of_either_half(bool v) {
+  const unsigned long long lanes = __ballot(v);
+  return (((unsigned)lanes | (unsigned)(lanes >> 32)) >> (threadIdx.x & 31)) & 1;
+}
+
 // a product with the sum of products before it, which is none
 template <typename T>
 __device__ __forceinline__ f32x16 mma_first(const u32x4& a, const u32x4& b) {
@@ -102,8 +107,10 @@ __device__ __forceinline__ f32x16 mma_first(const u32x4& a, const u32x4& b) {
 }
 
 // Scores become weights 2^(c s - m) of a row, which are added to its sum. What the exponents are relative to, m, need not be the maximum: as long as a tile's
-// weights add up to no more than kMostOfTile nothing overflows and nothing is lost, and it stays. Where they add up to more, as in the first tile, m becomes
-// the maximum so far and output and sum are multiplied. So the maximum is hardly ever formed.
+// weights add up to no more than kMostOfTile in either lane of a row it stays, and nothing is lost: output and sum are at most that many times too large, which values
+// below 2^115 leave room for (of larger ones an output may become infinite, and the row goes through the careful pass). Where they add up to more, as in the first
+// tile, the row's m becomes the maximum so far and its output and sum are multiplied. So the maximum is hardly ever formed. (Another row's m stays, and its weights are formed again
+// as they were: its bits do not depend on the rows beside it.)
 template <int NB, int DT>
 __device__ __forceinline__ void to_weights(f32x16 (&s)[NB], const float c, float& m, float& l, f32x16 (&o)[DT]) {
   f32x16 w[NB];
@@ -119,13 +126,16 @@ __device__ __forceinline__ void to_weights(f32x16 (&s)[NB], const float c, float
     return (part[0] + part[1]) + (part[2] + part[3]);
   };
   float sum = weights(m);   // (no key so far: m is -infinity, and the sum infinite or a NaN)
-  if (__any(!(sum <= kMostOfTile))) {
+  const bool many = !(sum <= kMostOfTile);
+  if (__any(many)) {
+    const bool grows = of_either_half(many);
     float top = s[0][0];
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int i = b ? 0 : 1; i < 16; ++i) top = __builtin_elementwise_maximum(top, s[b][i]);
-    const float grown = __builtin_elementwise_maximum(m, max_of_halves(top) * c), by = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
+    const float most = max_of_halves(top) * c, grown = grows ? __builtin_elementwise_maximum(m, most) : m;
+    const float by = !grows ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - grown);
     m = grown;
     l *= by;
 #pragma unroll
@@ -263,12 +273,14 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
   };
   const char* const kp = p.k + (long long)k0 * p.k_token + head * p.k_head;
   const char* const vp = p.v + (long long)k0 * p.v_token + head * p.v_head;
+  // (Said to be a scalar: where the compiler keeps it in a vector register, for the lanes' comparisons, every load below becomes a loop over the lanes' buffers.)
+  const int row_bytes = __builtin_amdgcn_readfirstlane(p.head_dim * E);
   auto issue = [&](int t, int buf) __attribute__((always_inline)) {   // (keys past the sequence's last arrive as zeros)
     const int left = min(nk - t * KT, KT) - 1;
     const __amdgpu_buffer_rsrc_t kb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(kp + (long long)t * KT * p.k_token), 0,
-                                                                        left * (int)p.k_token + p.head_dim * E, 0x00020000);
+                                                                        left * (int)p.k_token + row_bytes, 0x00020000);
     const __amdgpu_buffer_rsrc_t vb = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vp + (long long)t * KT * p.v_token), 0,
-                                                                        left * (int)p.v_token + p.head_dim * E, 0x00020000);
+                                                                        left * (int)p.v_token + row_bytes, 0x00020000);
     unsigned char* const dst = smem + buf * 2 * S::BYTES + wave * 1024;
 #pragma unroll
     for (int i = 0; i < LD; ++i)
@@ -298,7 +310,6 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 
   const float c = p.scale * kLog2e;
   f32x16 o[DT];
-  bool shares = false;   // the output is the mean already
   float m, l;   // what the exponents of c s are relative to, in powers of two; sum
   auto pass = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
@@ -424,10 +435,7 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
         });
       }
     }
-    if constexpr (careful) {
-      m *= c;
-      shares = true;
-    }
+    if constexpr (careful) m *= c;
   };
   // fp32 on the bf16 matrix cores: a value is the sum of three bf16 values, a product of two values the sum of the six largest partial products
   // (see conv_split.hpp): 192 cycles where the fp32 instructions take 512. Tiles of 32 keys pass through registers, where they are split, a tile ahead, into one
@@ -544,64 +552,68 @@ __global__ __launch_bounds__(256, (AttnShape<T, DP>::LDS <= 72 * 1024 ? 2 : 1)) 
 #pragma unroll
       for (int i = 0; i < 16; ++i) o[d][i] *= kSplitUnscale;
   };
-  // Also looked at: the sum of the weights. Relative to a score far from zero (see to_shares) all may vanish; else the largest is 2^-12 at
-  // least, and with the least sum here no other weight of more than 2^-62 of it is lost.
+  // The rows that a pass got right leave; whether there are others. Odd are an output that is not finite, a score that was not (low), and a sum of weights near
+  // zero: relative to a score far from zero (see to_shares) all weights may vanish, else the largest is at least 1. With the least sum here no weight of more than
+  // 2^-62 of the largest is lost. A later pass writes odd rows only, so that a row's bits do not depend on the rows beside it.
   constexpr float kLeastSum = 0x1p-64f;
-  auto any_odd = [&]() __attribute__((always_inline)) {
-    const float sum = sum_of_halves(l);
-    bool odd = !(low > -INFINITY) || (sees > t0 * KT && !(sum >= kLeastSum));
+  bool open = live;   // the row is still to be written
+  auto leave = [&](auto careful) __attribute__((always_inline)) {
+    const float sum = careful ? l : sum_of_halves(l);
+    bool odd = false;
+    if constexpr (!careful) {
+      odd = !(low > -INFINITY) || (sees > t0 * KT && !(sum >= kLeastSum));
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) < INFINITY);
-    return __syncthreads_or(odd && live) != 0;
-  };
-  // Weights of zero times an infinity or a NaN of a value that the row does not see are NaNs. They are rare, and looked for at the end only: then the
-  // keys are gone through again, one by one.
-  auto passes = [&]() __attribute__((always_inline)) {
-    get_ready();
-    low = 0.f;
-    pass(std::false_type{});
-    if (any_odd()) pass(std::true_type{});
+        for (int i = 0; i < 16; ++i) odd |= !(fabsf(o[d][i]) < INFINITY);
+      odd = of_either_half(odd);
+    }
+    if (open && !odd) {
+      const float by = careful ? 1.f : sum == 0.f ? 0.f : 1.f / sum;   // (no key: a row that sees none, or none of this part)
+      if (p.splits > 1) {
+        const long long rows = (long long)(p.hi - p.lo) * (p.heads_k * p.group);
+        const long long slot = blockIdx.y * rows + (at_row - p.lo) * (p.heads_k * p.group) + qh;
+        float* const to = p.part + slot * p.head_dim;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int at = d * 32 + j * 8 + half * 4;
+            if (at < p.head_dim) *(f32x4*)(to + at) = f32x4{o[d][j * 4] * by, o[d][j * 4 + 1] * by, o[d][j * 4 + 2] * by, o[d][j * 4 + 3] * by};
+          }
+        if (half == 0) *(float2*)(p.part + p.splits * rows * p.head_dim + slot * 2) = make_float2(m, sees > 0 ? sum : -1.f);
+      } else {
+        const float by_all = sum == 0.f ? NAN : by;   // (no seen score is one that fp32 holds)
+        char* const op = p.out + at_row * p.out_token + qh * p.out_head;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int at = d * 32 + j * 8 + half * 4;
+            if (at >= p.head_dim) continue;
+            alignas(16) T w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(sees > 0 ? o[d][j * 4 + e] * by_all : 0.f);
+            __builtin_memcpy(__builtin_assume_aligned(op + at * E, 4 * E), w, sizeof(w));
+          }
+        if (p.lse && half == 0) p.lse[(long long)qh * p.rows_q + at_row] = sees > 0 ? (m + log2f(sum)) * kLn2 : -INFINITY;
+      }
+    }
+    open = open && odd;
+    return careful ? 0 : __syncthreads_or(open);
   };
   if constexpr (S::PARTS) {
     pass_of_parts();
-    if (any_odd()) passes();
-  } else {
-    passes();
+    if (!leave(std::false_type{})) return;
   }
-  if (!shares) l = sum_of_halves(l);
-  if (!live) return;
-  const float by = shares ? 1.f : l == 0.f ? 0.f : 1.f / l;   // (no key: a row that sees none, or none of this part)
-
-  if (p.splits > 1) {
-    const long long rows = (long long)(p.hi - p.lo) * (p.heads_k * p.group);
-    const long long slot = blockIdx.y * rows + (at_row - p.lo) * (p.heads_k * p.group) + qh;
-    float* const to = p.part + slot * p.head_dim;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = d * 32 + j * 8 + half * 4;
-        if (at < p.head_dim) *(f32x4*)(to + at) = f32x4{o[d][j * 4] * by, o[d][j * 4 + 1] * by, o[d][j * 4 + 2] * by, o[d][j * 4 + 3] * by};
-      }
-    if (half == 0) *(float2*)(p.part + p.splits * rows * p.head_dim + slot * 2) = make_float2(m, sees > 0 ? l : -1.f);
-    return;
-  }
-  const float by_all = l == 0.f ? NAN : by;   // (no seen score is one that fp32 holds)
-  char* const op = p.out + at_row * p.out_token + qh * p.out_head;
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int at = d * 32 + j * 8 + half * 4;
-      if (at >= p.head_dim) continue;
-      alignas(16) T w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = from_f32<T>(sees > 0 ? o[d][j * 4 + e] * by_all : 0.f);
-      __builtin_memcpy(__builtin_assume_aligned(op + at * E, 4 * E), w, sizeof(w));
-    }
-  if (p.lse && half == 0) p.lse[(long long)qh * p.rows_q + at_row] = sees > 0 ? (m + log2f(l)) * kLn2 : -INFINITY;
+  // Weights of zero times an infinity or a NaN of a value that the row does not see are NaNs. They are rare, and looked for at the end only: then the
+  // keys are gone through again, one by one.
+  get_ready();
+  low = 0.f;
+  pass(std::false_type{});
+  if (!leave(std::false_type{})) return;
+  pass(std::true_type{});
+  leave(std::true_type{});
 }
 
 // Joins the parts of a row: a wavefront for each row and head, lane s has part s's maximum and sum. (A sum of -1: the row sees no key.)
