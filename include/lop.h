@@ -279,7 +279,7 @@ LOP_API int lop_plan_rowwise(const lop_rowwise_t* layers, int n_layers, int m, i
  * stream and may be captured into a graph. Everything they are told lies in a descriptor that is read during the call only. Strides
  * count elements. Pointers that the kernels move 16-byte vectors through start on a 16-byte boundary, and so does every
  * row and head behind them: strides are multiples of 16 bytes (where the extent is not 1); what is not is
- * LOP_ERR_INVALID_ARG, and so are strides that let rows or heads of an output overlap. Outputs do not overlap inputs unless a comment allows it. */
+ * LOP_ERR_INVALID_ARG, and so are strides that let rows, heads or scales of an output overlap. Outputs do not overlap inputs unless a comment allows it. */
 
 /* A matrix in 8-bit floating point (e4m3: 3 fraction bits, largest value 448, no infinities) with a scale for each block
  * of LOP_F8_BLOCK columns: q = x * (448 / a) rounded to nearest even, scale = a / 448, a = max(|x| over the block, 2^-64).
@@ -296,7 +296,7 @@ typedef struct {
   void* q;                  /* device, one byte a value                                                   */
   long long q_stride;
   float* scale;             /* device, ceil(m / block_rows) x ceil(k / LOP_F8_BLOCK)                      */
-  long long scale_row, scale_col; /* strides of scale; scale_row == 1 is what lop_rowwise_f8 reads fastest */
+  long long scale_row, scale_col; /* strides of scale: no two scales share a place; scale_row == 1 is what lop_rowwise_f8 reads fastest */
 } lop_quantize_t;
 /* rows: of x; with block_rows == LOP_F8_BLOCK lo is a multiple of it, and hi one, or m. */
 LOP_API int lop_quantize_blocks(const lop_quantize_t* op, lop_rows_t rows, void* stream);

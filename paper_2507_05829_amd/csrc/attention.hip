@@ -742,7 +742,7 @@ extern "C" int lop_attention(const lop_attention_t* op, lop_rows_t rows, void* s
     return LOP_ERR_INVALID_ARG;
   if (op->rows_k > 0 && (!good(op->k, op->k_token, op->k_head, op->rows_k, op->heads_k) || !good(op->v, op->v_token, op->v_head, op->rows_k, op->heads_k)))
     return LOP_ERR_INVALID_ARG;
-  if (!apart(op->out_token, op->head_dim, op->rows_q) || !apart(op->out_head, op->head_dim, op->heads_q)) return LOP_ERR_INVALID_ARG;
+  if (!apart(op->head_dim, op->out_token, op->rows_q, op->out_head, op->heads_q)) return LOP_ERR_INVALID_ARG;
   if (!op->q_offsets || !op->k_begin || !op->k_end) return LOP_ERR_INVALID_ARG;
   if (((uintptr_t)op->q_offsets | (uintptr_t)op->k_begin | (uintptr_t)op->k_end | (uintptr_t)op->lse) & 3 || !aligned16(op->workspace)) return LOP_ERR_INVALID_ARG;
   // (a tile's keys are one buffer: its rows lie behind one another, and offsets in it are 32 bits)

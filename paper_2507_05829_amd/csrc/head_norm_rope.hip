@@ -194,8 +194,8 @@ extern "C" int lop_head_norm_rope(const lop_head_norm_rope_t* op, lop_rows_t row
       !good(op->k, op->k_token, op->k_head, op->heads_k) || !good(op->k_out, op->k_out_token, op->k_out_head, op->heads_k))
     return LOP_ERR_INVALID_ARG;
   for (int i = 0; i < 2; ++i)   // an output's heads do not overlap
-    if (const int heads = i ? op->heads_k : op->heads_q; heads > 0 && (!apart(i ? op->k_out_token : op->q_out_token, op->head_dim, op->tokens) ||
-                                                                      !apart(i ? op->k_out_head : op->q_out_head, op->head_dim, heads)))
+    if (const int heads = i ? op->heads_k : op->heads_q; heads > 0 && !apart(op->head_dim, i ? op->k_out_token : op->q_out_token, op->tokens,
+                                                                            i ? op->k_out_head : op->q_out_head, heads))
       return LOP_ERR_INVALID_ARG;
   if (!aligned16(op->q_weight) || !aligned16(op->k_weight)) return LOP_ERR_INVALID_ARG;
   if (op->rot_dim > 0 && (!op->positions || ((uintptr_t)op->positions & 3) || !op->freq || !aligned16(op->freq))) return LOP_ERR_INVALID_ARG;

@@ -154,6 +154,6 @@ extern "C" int lop_quantize_blocks(const lop_quantize_t* op, lop_rows_t rows, vo
   if (!op->x || !op->q || !op->scale || !aligned16(op->x) || !aligned16(op->q) || ((uintptr_t)op->scale & 3)) return LOP_ERR_INVALID_ARG;
   if (!whole_vectors(op->x_stride, dtype_bytes(op->dtype), op->m > 1) || !whole_vectors(op->q_stride, 1, op->m > 1) || !apart(op->q_stride, op->k, op->m))
     return LOP_ERR_INVALID_ARG;
-  if (op->scale_row < 0 || op->scale_col < 0) return LOP_ERR_INVALID_ARG;
+  if (op->scale_row < 0 || op->scale_col < 0 || !apart(1, op->scale_row, ceil_div(op->m, op->block_rows), op->scale_col, ceil_div(op->k, kBlock))) return LOP_ERR_INVALID_ARG;
   return op->dtype == LOP_BF16 ? quantize<__bf16>(op, rows, (hipStream_t)stream) : quantize<float>(op, rows, (hipStream_t)stream);
 }
