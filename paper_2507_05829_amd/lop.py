@@ -14,6 +14,7 @@ import ctypes
 import os
 import struct
 from ctypes import POINTER, Structure, byref, c_char_p, c_double, c_float, c_int, c_longlong, c_size_t, c_uint, c_ulonglong, c_void_p
+from operator import index
 from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
@@ -419,8 +420,10 @@ def lop_measure_ceilings() -> lop_ceilings_t:
 
 
 def _rows_word(lo: int, hi: int) -> int:
-    """A lop_rows_t that is passed by value, as the register it travels in (two 32-bit integers, the first in the low half)."""
-    return c_longlong((lo & 0xffffffff) | (hi & 0xffffffff) << 32).value
+    """A lop_rows_t that is passed by value, as the register it travels in (two 32-bit integers, the first in the low half). Numbers that
+    they do not hold are no band's: -1, as every negative number."""
+    lo, hi = index(lo), index(hi)
+    return -1 if (lo | hi) >> 31 else lo | hi << 32
 
 
 def lop_quantize_blocks(op: lop_quantize_t, rows: Tuple[int, int], stream=None) -> None:

@@ -1,0 +1,75 @@
+"""What the torch bindings of the transformer operators say to tensors, bands and numbers that do not fit, on the CPU: everything here is refused
+in front of the library's launch. (The current device is told to be the CPU's, -1, for the checks to get as far.)"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2507_05829_amd import lop
+from test_operators_host import BAND, attention_op, product_op, quantize_op, rope_op
+
+BANDS = [(0, 1 << 32), (1 << 32, (1 << 32) + 5), (0, (1 << 32) + 5), (0, 1 << 31), (-(1 << 32), 5), (-(1 << 40), -(1 << 40) + 3), (-1, 3), (np.int64(0), np.int64(1 << 33))]
+
+
+@pytest.mark.parametrize("rows", BANDS, ids=str)
+@pytest.mark.parametrize("call,op", [(lop.lop_quantize_blocks, quantize_op), (lop.lop_rowwise_f8, product_op), (lop.lop_head_norm_rope, rope_op),
+                                     (lop.lop_attention, attention_op), (lop.lop_attention_workspace, attention_op)], ids=lambda c: c.__name__)
+def test_bands_of_more_than_32_bits_do_not_wrap(call, op, rows):
+    with pytest.raises(lop.LopError) as e:
+        call(op(), rows)
+    assert e.value.code == BAND
+
+
+def test_bands_of_numpy_numbers():
+    for t in (np.int32, np.int64, np.uint8):
+        lop.lop_quantize_blocks(quantize_op(), (t(7), t(7)))        # empty: nothing is enqueued
+    with pytest.raises(TypeError):
+        lop.lop_quantize_blocks(quantize_op(), (0.0, 5.0))
+
+
+# ------------------------------------------------------------------ tensors
+
+
+class Calls:
+    """Arguments of each operator's call, by name, that fit."""
+
+    def __init__(self):
+        f8, b16, i32 = torch.float8_e4m3fn, torch.bfloat16, torch.int32
+        zeros = torch.zeros
+        self.of = {
+            "quantize_blocks": dict(x=zeros(3, 128, dtype=b16), q=zeros(3, 128).to(f8), scale=zeros(3, 1)),
+            "rowwise_f8": dict(x=zeros(3, 128).to(f8), x_scale=zeros(3, 1), w=zeros(5, 128).to(f8), w_scale=zeros(1, 1), bias=zeros(5), residual=zeros(3, 5, dtype=b16),
+                               y=zeros(3, 5, dtype=b16)),
+            "head_norm_rope": dict(q=zeros(3, 2, 64, dtype=b16), k=zeros(3, 1, 64, dtype=b16), positions=zeros(3, dtype=i32), freq=zeros(32), q_weight=zeros(64), k_weight=zeros(64),
+                                   q_out=zeros(3, 2, 64, dtype=b16), k_out=zeros(3, 1, 64, dtype=b16)),
+            "attention": dict(q=zeros(3, 2, 64, dtype=b16), k=zeros(9, 1, 64, dtype=b16), v=zeros(9, 1, 64, dtype=b16), q_offsets=zeros(2, dtype=i32), k_begin=zeros(1, dtype=i32),
+                              k_end=zeros(1, dtype=i32), scale=0.125, out=zeros(3, 2, 64, dtype=b16), lse=zeros(2, 3)),
+        }
+
+
+@pytest.fixture
+def on_the_cpu(monkeypatch):
+    """The checks take the CPU for the current device; what passes them is kept from the library."""
+    monkeypatch.setattr(lop, "_current_device", lambda: -1)
+    monkeypatch.setattr(lop, "_current_stream", lambda device: 0)
+
+    class Library:
+        def __init__(self):
+            self.reached = []
+
+        def __getattr__(self, name):
+            def call(*args):
+                self.reached.append(name)
+                return 0
+            return call
+    library = Library()
+    monkeypatch.setattr(lop, "_lib", library)
+    return library
+
+
+NAMES = list(Calls().of)
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_what_fits_reaches_the_library(name, on_the_cpu):
+    getattr(lop, name)(**Calls().of[name])
+    assert on_the_cpu.reached == ["lop_" + name]
