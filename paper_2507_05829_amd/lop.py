@@ -592,7 +592,7 @@ class Plan:
 # lop_quantize_blocks, lop_rowwise_f8, lop_head_norm_rope and lop_attention on tensors: the descriptor is read off
 # them. They run on torch's current stream of the current device, where every tensor has to be; outputs that are not
 # passed are allocated there. `rows`: the band of output rows that is computed (lo, hi), everything if None. Forward
-# only: a tensor that wants a gradient is refused while gradients are recorded. Shapes and types that do not fit
+# only: a tensor that wants a gradient is refused while gradients are recorded, and one with a tangent always. Shapes and types that do not fit
 # raise ValueError, what the library refuses LopError.
 
 # (the library's host code also runs beside a stand-in for torch that has no tensors)
@@ -604,7 +604,7 @@ def _bad(name: str, what: str):
     raise ValueError(f"{name}: {what}")
 
 
-def _refuse(device: int, grad: bool, *named) -> None:
+def _refuse(device: int, grad: int, *named) -> None:
     """Says what is wrong with the first of (name, tensor, type, shape, rows) that does not fit: `shape` None for any, or with None
     for any extent; `rows`: the values of a row lie next to one another (2: all of them do)."""
     for name, t, dtype, shape, rows in named:
@@ -616,8 +616,10 @@ def _refuse(device: int, grad: bool, *named) -> None:
             _bad(name, f"{tuple(shape)} is wanted, not {tuple(t.shape)}")
         if t.get_device() != device:
             _bad(name, f"on {t.device}, not on the current device ({device})")
-        if grad and t.requires_grad:
+        if grad & 1 and t.requires_grad:
             _bad(name, "forward only, but the tensor wants a gradient")
+        if grad & 2 and _forward_ad.unpack_dual(t).tangent is not None:
+            _bad(name, "no derivatives, but the tensor has a tangent")
         if rows == 2 and not t.is_contiguous():
             _bad(name, "dense memory is wanted")
         if rows and t.stride(-1) != 1 and t.shape[-1] > 1 and t.numel() > 0:
@@ -637,14 +639,15 @@ def _dims(name: str, t, n: int):
     return t.shape
 
 
-_current_device, _current_stream, _grad_enabled = (
-    (torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, torch.is_grad_enabled) if _TYPES else (None, None, None))
+_current_device, _current_stream, _grad_enabled, _forward_ad = (
+    (torch.cuda.current_device, torch._C._cuda_getCurrentRawStream, torch.is_grad_enabled, torch.autograd.forward_ad) if _TYPES else (None,) * 4)
 
 
 def _here():
-    """The current device, its current stream, whether gradients are recorded."""
+    """The current device, its current stream, and 1 where gradients are recorded + 2 where tensors may have tangents (a level of forward-mode
+    derivatives is open: then _refuse looks at every tensor)."""
     device = _current_device()
-    return device, _current_stream(device), _grad_enabled()
+    return device, _current_stream(device), _grad_enabled() + 2 * (_forward_ad._current_level >= 0)
 
 
 # Each function first asks in one expression whether everything fits, and goes through the tensors one by one only where
@@ -673,7 +676,7 @@ def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
     xs, qs, ss = x.stride(), q.stride(), scale.stride()
     if (q.dtype is not _F8 or scale.dtype is not torch.float32 or q.shape != shape or scale.shape != blocks
             or x.get_device() != device or q.get_device() != device or scale.get_device() != device
-            or (grad and (x.requires_grad or q.requires_grad or scale.requires_grad)) or xs[1] != 1 or qs[1] != 1):
+            or grad > 1 or (grad and (x.requires_grad or q.requires_grad or scale.requires_grad)) or xs[1] != 1 or qs[1] != 1):
         _refuse(device, grad, ("x", x, x.dtype, None, 1), ("q", q, _F8, shape, 1), ("scale", scale, torch.float32, blocks, 0))
     op = _QUANTIZE.pack(m, k, code, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), ss[0], ss[1])
     e = _lib.lop_quantize_blocks(op, m << 32 if rows is None else _rows_word(*rows), stream)
@@ -701,7 +704,7 @@ def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=No
             or x_scale.shape != (m, kb) or w_scale.shape != (-(-n // LOP_F8_BLOCK), kb) or y.shape != (m, n)
             or x.get_device() != device or w.get_device() != device or x_scale.get_device() != device
             or w_scale.get_device() != device or y.get_device() != device
-            or (grad and (x.requires_grad or w.requires_grad or x_scale.requires_grad or w_scale.requires_grad or y.requires_grad))
+            or grad > 1 or (grad and (x.requires_grad or w.requires_grad or x_scale.requires_grad or w_scale.requires_grad or y.requires_grad))
             or xs[1] != 1 or ws[1] != 1 or ys[1] != 1):
         _refuse(device, grad, ("x", x, _F8, None, 1), ("w", w, _F8, (n, k), 1), ("x_scale", x_scale, f32, (m, kb), 0),
                 ("w_scale", w_scale, f32, (-(-n // LOP_F8_BLOCK), kb), 0), ("y", y, dtype, (m, n), 1))
@@ -733,7 +736,7 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
         q_out = torch.empty(shape, dtype=dtype, device=q.device)
     qs, qos = q.stride(), q_out.stride()
     if (q_out.dtype is not dtype or q_out.shape != shape or q.get_device() != device or q_out.get_device() != device
-            or (grad and (q.requires_grad or q_out.requires_grad)) or qs[2] != 1 or qos[2] != 1):
+            or grad > 1 or (grad and (q.requires_grad or q_out.requires_grad)) or qs[2] != 1 or qos[2] != 1):
         _refuse(device, grad, ("q", q, dtype, None, 1), ("q_out", q_out, dtype, shape, 1))
     hk = k_at = k_out_at = 0
     ks = kos = (0, 0)
@@ -744,7 +747,7 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
             k_out = torch.empty(k_shape, dtype=dtype, device=q.device)
         ks, kos = k.stride(), k_out.stride()
         if (k.dtype is not dtype or k_out.dtype is not dtype or k_shape[0] != tokens or k_shape[2] != d or k_out.shape != k_shape
-                or k.get_device() != device or k_out.get_device() != device or (grad and (k.requires_grad or k_out.requires_grad))
+                or k.get_device() != device or k_out.get_device() != device or grad > 1 or (grad and (k.requires_grad or k_out.requires_grad))
                 or ks[2] != 1 or kos[2] != 1):
             _refuse(device, grad, ("k", k, dtype, (tokens, hk, d), 1), ("k_out", k_out, dtype, k_shape, 1))
         k_at, k_out_at = k.data_ptr(), k_out.data_ptr()
@@ -752,19 +755,19 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
     if freq is not None and positions is not None:
         turns = freq.numel()
         if (positions.dtype is not torch.int32 or freq.dtype is not f32 or freq.dim() != 1 or positions.shape != (tokens,)
-                or positions.get_device() != device or freq.get_device() != device or freq.requires_grad
+                or positions.get_device() != device or freq.get_device() != device or grad > 1 or freq.requires_grad
                 or positions.stride(0) != 1 or freq.stride(0) != 1):
             _refuse(device, grad, ("positions", positions, torch.int32, (tokens,), 1), ("freq", freq, f32, (None,), 1))
         positions_at, freq_at = positions.data_ptr(), freq.data_ptr()
     elif freq is not None or positions is not None:
         _bad("positions", "they and freq go together")
     if q_weight is not None:
-        if (q_weight.dtype is not f32 or q_weight.shape != (d,) or q_weight.get_device() != device or q_weight.requires_grad
+        if (q_weight.dtype is not f32 or q_weight.shape != (d,) or q_weight.get_device() != device or grad > 1 or q_weight.requires_grad
                 or q_weight.stride(0) != 1):
             _refuse(device, grad, ("q_weight", q_weight, f32, (d,), 1))
         q_weight_at = q_weight.data_ptr()
     if k_weight is not None:
-        if (k_weight.dtype is not f32 or k_weight.shape != (d,) or k_weight.get_device() != device or k_weight.requires_grad
+        if (k_weight.dtype is not f32 or k_weight.shape != (d,) or k_weight.get_device() != device or grad > 1 or k_weight.requires_grad
                 or k_weight.stride(0) != 1):
             _refuse(device, grad, ("k_weight", k_weight, f32, (d,), 1))
         k_weight_at = k_weight.data_ptr()
@@ -796,7 +799,7 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
             or k_end.dtype is not i32 or k_shape[2] != d or v.shape != k_shape or out.shape != shape or q_offsets.shape != (seqs + 1,)
             or k_end.shape != (seqs,) or q.get_device() != device or k.get_device() != device or v.get_device() != device
             or out.get_device() != device or q_offsets.get_device() != device or k_begin.get_device() != device
-            or k_end.get_device() != device or (grad and (q.requires_grad or k.requires_grad or v.requires_grad or out.requires_grad))
+            or k_end.get_device() != device or grad > 1 or (grad and (q.requires_grad or k.requires_grad or v.requires_grad or out.requires_grad))
             or qs[2] != 1 or ks[2] != 1 or vs[2] != 1 or os_[2] != 1 or q_offsets.stride(0) != 1 or k_begin.stride(0) != 1
             or k_end.stride(0) != 1):
         _refuse(device, grad, ("q", q, dtype, None, 1), ("k", k, dtype, (rows_k, hk, d), 1), ("v", v, dtype, k_shape, 1),

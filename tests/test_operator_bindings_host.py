@@ -73,3 +73,34 @@ NAMES = list(Calls().of)
 def test_what_fits_reaches_the_library(name, on_the_cpu):
     getattr(lop, name)(**Calls().of[name])
     assert on_the_cpu.reached == ["lop_" + name]
+
+
+PAIRS = [(name, key) for name, args in Calls().of.items() for key, t in args.items() if isinstance(t, torch.Tensor)]
+
+
+@pytest.mark.parametrize("name,key", [(n, k) for n, k in PAIRS if Calls().of[n][k].is_floating_point()])
+@pytest.mark.parametrize("recorded", [True, False])
+def test_tensors_with_a_tangent_are_refused(name, key, recorded, on_the_cpu):
+    """Forward-mode derivatives would be dropped; gradients need not be recorded for them."""
+    args, fw = Calls().of[name], torch.autograd.forward_ad
+    plain = dict(args)
+    with torch.set_grad_enabled(recorded), fw.dual_level():
+        getattr(lop, name)(**plain)                              # no tensor has one: as ever
+        t = args[key]
+        args[key] = fw.make_dual(t, t.clone())
+        with pytest.raises(ValueError, match=f"{key}: .*tangent"):
+            getattr(lop, name)(**args)
+    assert on_the_cpu.reached == ["lop_" + name]
+    getattr(lop, name)(**plain)
+
+
+@pytest.mark.parametrize("name,key", [(n, k) for n, k in PAIRS if Calls().of[n][k].is_floating_point()])
+def test_tensors_that_want_a_gradient_are_refused_while_it_is_recorded(name, key, on_the_cpu):
+    args = Calls().of[name]
+    args[key].requires_grad_()
+    with pytest.raises(ValueError, match=f"{key}: .*gradient"):
+        getattr(lop, name)(**args)
+    assert not on_the_cpu.reached
+    with torch.no_grad():
+        getattr(lop, name)(**args)
+    assert on_the_cpu.reached == ["lop_" + name]
