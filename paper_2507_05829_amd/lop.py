@@ -650,6 +650,10 @@ def _here():
     return device, _current_stream(device), _grad_enabled() + 2 * (_forward_ad._current_level >= 0)
 
 
+def _no_number(e: struct.error):
+    raise ValueError(f"a size, stride or factor that the library does not hold: {e}") from e
+
+
 # Each function first asks in one expression whether everything fits, and goes through the tensors one by one only where
 # something does not: a call of one token is bound by the host. (The descriptors are packed for the same reason:
 # filling the fields of a ctypes structure takes four times as long.)
@@ -678,7 +682,10 @@ def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
             or x.get_device() != device or q.get_device() != device or scale.get_device() != device
             or grad > 1 or (grad and (x.requires_grad or q.requires_grad or scale.requires_grad)) or xs[1] != 1 or qs[1] != 1):
         _refuse(device, grad, ("x", x, x.dtype, None, 1), ("q", q, _F8, shape, 1), ("scale", scale, torch.float32, blocks, 0))
-    op = _QUANTIZE.pack(m, k, code, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), ss[0], ss[1])
+    try:
+        op = _QUANTIZE.pack(m, k, code, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), ss[0], ss[1])
+    except struct.error as e:
+        _no_number(e)
     e = _lib.lop_quantize_blocks(op, m << 32 if rows is None else _rows_word(*rows), stream)
     if e:
         _check(e, "lop_quantize_blocks")
@@ -715,8 +722,11 @@ def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=No
     if residual is not None:
         _refuse(device, grad, ("residual", residual, dtype, (m, n), 1))
         residual_at, residual_stride = residual.data_ptr(), residual.stride(0)
-    op = _ROWWISE_F8.pack(m, n, k, code, _ACTS[act], x.data_ptr(), xs[0], x_scale.data_ptr(), xss[0], xss[1], w.data_ptr(), ws[0],
-                          w_scale.data_ptr(), wss[0], wss[1], bias_at, residual_at, residual_stride, y.data_ptr(), ys[0])
+    try:
+        op = _ROWWISE_F8.pack(m, n, k, code, _ACTS[act], x.data_ptr(), xs[0], x_scale.data_ptr(), xss[0], xss[1], w.data_ptr(), ws[0],
+                              w_scale.data_ptr(), wss[0], wss[1], bias_at, residual_at, residual_stride, y.data_ptr(), ys[0])
+    except struct.error as e:
+        _no_number(e)
     e = _lib.lop_rowwise_f8(op, m << 32 if rows is None else _rows_word(*rows), stream)
     if e:
         _check(e, "lop_rowwise_f8")
@@ -771,9 +781,12 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
                 or k_weight.stride(0) != 1):
             _refuse(device, grad, ("k_weight", k_weight, f32, (d,), 1))
         k_weight_at = k_weight.data_ptr()
-    op = _HEAD_NORM_ROPE.pack(tokens, hq, hk, d, 2 * turns, interleaved, code, eps, amplitude, q.data_ptr(), qs[0], qs[1],
-                              k_at, ks[0], ks[1], q_out.data_ptr(), qos[0], qos[1], k_out_at, kos[0], kos[1],
-                              q_weight_at, k_weight_at, positions_at, freq_at)
+    try:
+        op = _HEAD_NORM_ROPE.pack(tokens, hq, hk, d, 2 * turns, interleaved, code, eps, amplitude, q.data_ptr(), qs[0], qs[1],
+                                  k_at, ks[0], ks[1], q_out.data_ptr(), qos[0], qos[1], k_out_at, kos[0], kos[1],
+                                  q_weight_at, k_weight_at, positions_at, freq_at)
+    except struct.error as e:
+        _no_number(e)
     e = _lib.lop_head_norm_rope(op, tokens << 32 if rows is None else _rows_word(*rows), stream)
     if e:
         _check(e, "lop_head_norm_rope")
@@ -805,7 +818,7 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
         _refuse(device, grad, ("q", q, dtype, None, 1), ("k", k, dtype, (rows_k, hk, d), 1), ("v", v, dtype, k_shape, 1),
                 ("out", out, dtype, shape, 1), ("q_offsets", q_offsets, i32, (seqs + 1,), 1), ("k_begin", k_begin, i32, (seqs,), 1),
                 ("k_end", k_end, i32, (seqs,), 1))
-    lse_at = workspace_at = workspace_bytes = 0
+    lse_at = 0
     if lse is not None:
         _refuse(device, grad, ("lse", lse, torch.float32, (hq, rows_q), 2))
         lse_at = lse.data_ptr()
@@ -814,15 +827,19 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
     band = rows_q << 32 if rows is None else _rows_word(*rows)
     fields = (code, hq, hk, d, seqs, rows_q, rows_k, max_keys, causal, scale, q.data_ptr(), qs[0], qs[1], k.data_ptr(), ks[0], ks[1],
               v.data_ptr(), vs[0], vs[1], out.data_ptr(), os_[0], os_[1], q_offsets.data_ptr(), k_begin.data_ptr(), k_end.data_ptr(), lse_at)
+    try:
+        op = _ATTENTION.pack(*fields, 0, 0)
+    except struct.error as e:
+        _no_number(e)
     if workspace is None and max_keys >= (LOP_ATTENTION_CUT_F32 if code == LOP_F32 else LOP_ATTENTION_CUT):
         n = c_ulonglong(0)
-        _check(_lib.lop_attention_workspace(_ATTENTION.pack(*fields, 0, 0), band, byref(n)), "lop_attention_workspace")
+        _check(_lib.lop_attention_workspace(op, band, byref(n)), "lop_attention_workspace")
         if n.value:
             workspace = torch.empty(n.value, dtype=torch.uint8, device=q.device)
     if workspace is not None:
         _refuse(device, grad, ("workspace", workspace, torch.uint8, (None,), 2))
-        workspace_at, workspace_bytes = workspace.data_ptr(), workspace.numel()
-    e = _lib.lop_attention(_ATTENTION.pack(*fields, workspace_at, workspace_bytes), band, stream)
+        op = _ATTENTION.pack(*fields, workspace.data_ptr(), workspace.numel())
+    e = _lib.lop_attention(op, band, stream)
     if e:
         _check(e, "lop_attention")
     return out

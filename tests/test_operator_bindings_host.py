@@ -104,3 +104,23 @@ def test_tensors_that_want_a_gradient_are_refused_while_it_is_recorded(name, key
     with torch.no_grad():
         getattr(lop, name)(**args)
     assert on_the_cpu.reached == ["lop_" + name]
+
+
+@pytest.mark.parametrize("name,change", [
+    ("quantize_blocks", lambda a: {k: t[:1].expand(1 << 31, -1) for k, t in a.items()}),
+    ("rowwise_f8", lambda a: {k: t[:1].expand(1 << 31, -1) if k in ("x", "x_scale", "residual", "y") else t for k, t in a.items()}),
+    ("head_norm_rope", lambda a: dict({k: t[:1].expand(1 << 31, -1, -1) if t.dim() == 3 else t for k, t in a.items()}, positions=None, freq=None)),
+    ("head_norm_rope", lambda a: dict(a, eps="1")), ("attention", lambda a: dict(a, scale=None)),
+    ("attention", lambda a: {k: t[:1].expand(1 << 31, -1, -1) if k in ("k", "v") else t for k, t in a.items()}),
+    ("attention", lambda a: dict(a, max_keys=1 << 31)), ("attention", lambda a: dict(a, max_keys=-(1 << 40)))])
+def test_numbers_that_the_library_does_not_hold_are_refused(name, change, on_the_cpu):
+    with pytest.raises(ValueError):
+        getattr(lop, name)(**change(Calls().of[name]))
+    assert not on_the_cpu.reached
+
+
+def test_a_workspace_is_asked_for_and_passed(on_the_cpu):
+    args = Calls().of["attention"]
+    lop.attention(**args, max_keys=lop.LOP_ATTENTION_CUT)
+    lop.attention(**args, max_keys=1 << 20, workspace=torch.empty(64, dtype=torch.uint8))
+    assert on_the_cpu.reached == ["lop_attention_workspace", "lop_attention", "lop_attention"]
