@@ -15,6 +15,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
 
 #include "act.hpp"
 #include "conv_common.hpp"
@@ -606,6 +607,27 @@ int choose(long long m, long long n, int k, bool f32) {
   return best;
 }
 
+struct Kernel {
+  void (*run)(const F8Params);
+  const char* name;   // of the instance, with %s for the type of its results
+  int bm, bn, threads;
+  long long most;     // workgroups
+};
+template <typename T>
+Kernel kernel_of(long long m, long long n, int k) {
+  constexpr long long all = 1LL << 31;
+  switch (choose(m, n, k, sizeof(T) == 4)) {
+    case 0: return {rowwise_f8_few_kernel<T, 1, 2, 8>, "rowwise_f8_few_kernel<%s, 1, 2, 8>", 16, 32, 512, all};
+    case 1: return {rowwise_f8_few_kernel<T, 2, 2, 8>, "rowwise_f8_few_kernel<%s, 2, 2, 8>", 32, 32, 512, all};
+    case 2: return {rowwise_f8_few_kernel<T, 2, 4, 4>, "rowwise_f8_few_kernel<%s, 2, 4, 4>", 32, 64, 256, all};
+    case 3: return {rowwise_f8_kernel<T, 64, 128, 1, 2, 2>, "rowwise_f8_kernel<%s, 64, 128, 1, 2, 2>", 64, 128, 256, all};
+    case 4: break;
+    default:   // (not chosen for fp32)
+      if constexpr (sizeof(T) == 2) return {rowwise_f8_kernel<T, 256, 256, 4, 2, 1>, "rowwise_f8_kernel<%s, 256, 256, 4, 2, 1>", 256, 256, 512, kCus};
+  }
+  return {rowwise_f8_kernel<T, 128, 128, 2, 2, 1>, "rowwise_f8_kernel<%s, 128, 128, 2, 2, 1>", 128, 128, 256, all};
+}
+
 template <typename T>
 int rowwise_f8(const lop_rowwise_f8_t* op, lop_rows_t rows, hipStream_t stream) {
   constexpr int E = (int)sizeof(T);
@@ -621,25 +643,19 @@ int rowwise_f8(const lop_rowwise_f8_t* op, lop_rows_t rows, hipStream_t stream) 
   const uintptr_t bits = (uintptr_t)p.y | (uintptr_t)p.res | (uintptr_t)p.y_stride | (uintptr_t)(p.res ? p.res_stride : 0);
   p.vectors = bits % 16 == 0 && op->n % (16 / E) == 0;
   const int rows_in = rows.hi - rows.lo;
-  auto launch = [&](auto* kernel, int bm, int bn, int threads, long long most = 1LL << 31) -> int {
-    const long long mx = ceil_div(rows_in, bm), ny = ceil_div(op->n, bn);
-    if (mx * ny > launch_blocks(threads) || ny > 65535) return LOP_ERR_UNSUPPORTED;
-    p.mx = (int)mx; p.ny = (int)ny;
-    p.by_group = make_fastdiv(kGroupM * p.ny);
-    LOP_HIP(launch_kernel(kernel, dim3((unsigned)std::min(mx * ny, most)), dim3(threads), stream, nullptr, p));
-    return LOP_OK;
-  };
-  switch (choose(rows_in, op->n, op->k, sizeof(T) == 4)) {
-    case 0: return launch(rowwise_f8_few_kernel<T, 1, 2, 8>, 16, 32, 512);
-    case 1: return launch(rowwise_f8_few_kernel<T, 2, 2, 8>, 32, 32, 512);
-    case 2: return launch(rowwise_f8_few_kernel<T, 2, 4, 4>, 32, 64, 256);
-    case 3: return launch(rowwise_f8_kernel<T, 64, 128, 1, 2, 2>, 64, 128, 256);
-    case 4: return launch(rowwise_f8_kernel<T, 128, 128, 2, 2, 1>, 128, 128, 256);
-    default:
-      if constexpr (sizeof(T) == 2) return launch(rowwise_f8_kernel<T, 256, 256, 4, 2, 1>, 256, 256, 512, kCus);
-      return LOP_ERR_UNSUPPORTED;   // (not chosen)
-  }
+  const Kernel kernel = kernel_of<T>(rows_in, op->n, op->k);
+  const long long mx = ceil_div(rows_in, kernel.bm), ny = ceil_div(op->n, kernel.bn);
+  if (mx * ny > launch_blocks(kernel.threads) || ny > 65535) return LOP_ERR_UNSUPPORTED;
+  p.mx = (int)mx; p.ny = (int)ny;
+  p.by_group = make_fastdiv(kGroupM * p.ny);
+  LOP_HIP(launch_kernel(kernel.run, dim3((unsigned)std::min(mx * ny, kernel.most)), dim3(kernel.threads), stream, nullptr, p));
   return LOP_OK;
+}
+
+int check_sizes(const lop_rowwise_f8_t* op, lop_rows_t rows) {
+  if (!op || op->m < 0 || op->n < 1 || op->k < 1) return LOP_ERR_INVALID_ARG;
+  if (!known_dtype(op->dtype) || op->k % 16 || op->act < LOP_ACT_NONE || op->act > LOP_ACT_RELU6) return LOP_ERR_UNSUPPORTED;
+  return check_band(rows, op->m);
 }
 
 }  // namespace
@@ -647,9 +663,7 @@ int rowwise_f8(const lop_rowwise_f8_t* op, lop_rows_t rows, hipStream_t stream) 
 
 extern "C" int lop_rowwise_f8(const lop_rowwise_f8_t* op, lop_rows_t rows, void* stream) {
   using namespace lop;
-  if (!op || op->m < 0 || op->n < 1 || op->k < 1) return LOP_ERR_INVALID_ARG;
-  if (!known_dtype(op->dtype) || op->k % 16 || op->act < LOP_ACT_NONE || op->act > LOP_ACT_RELU6) return LOP_ERR_UNSUPPORTED;
-  if (const int e = check_band(rows, op->m)) return e;
+  if (const int e = check_sizes(op, rows)) return e;
   if (rows.lo == rows.hi) return LOP_OK;
   const size_t E = dtype_bytes(op->dtype);
   if (!op->x || !op->w || !op->x_scale || !op->w_scale || !op->y || !aligned16(op->x) || !aligned16(op->w)) return LOP_ERR_INVALID_ARG;
@@ -669,4 +683,16 @@ extern "C" int lop_rowwise_f8(const lop_rowwise_f8_t* op, lop_rows_t rows, void*
       (op->n > kBlock && op->w_scale_row > far / 4) || op->k > far)
     return LOP_ERR_UNSUPPORTED;
   return op->dtype == LOP_BF16 ? rowwise_f8<__bf16>(op, rows, (hipStream_t)stream) : rowwise_f8<float>(op, rows, (hipStream_t)stream);
+}
+
+extern "C" int lop_rowwise_f8_kernel(const lop_rowwise_f8_t* op, lop_rows_t rows, char* name, size_t size) {
+  using namespace lop;
+  if (!name || size == 0) return LOP_ERR_INVALID_ARG;
+  name[0] = 0;
+  if (const int e = check_sizes(op, rows)) return e;
+  const int m = rows.hi - rows.lo;
+  if (m == 0) return LOP_OK;
+  if (op->dtype == LOP_BF16) snprintf(name, size, kernel_of<__bf16>(m, op->n, op->k).name, "__bf16");
+  else snprintf(name, size, kernel_of<float>(m, op->n, op->k).name, "float");
+  return LOP_OK;
 }

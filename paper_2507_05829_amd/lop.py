@@ -57,7 +57,7 @@ EXPORTS = [
     "lop_last_hip_error", "lop_plan_layer_kernel", "lop_profile_chain", "lop_copy_chain",
     "lop_plan_band_compute_rows", "lop_plan_rowwise", "lop_loss_eval", "lop_loss_solve",
     "lop_run_two_party", "lop_measure_ceilings", "lop_run_chain_static", "lop_debug_guard_check",
-    "lop_quantize_blocks", "lop_rowwise_f8", "lop_head_norm_rope", "lop_attention_workspace", "lop_attention",
+    "lop_quantize_blocks", "lop_rowwise_f8", "lop_rowwise_f8_kernel", "lop_head_norm_rope", "lop_attention_workspace", "lop_attention",
 ]
 
 
@@ -192,6 +192,7 @@ def _load() -> ctypes.CDLL:
         "lop_measure_ceilings": (c_int, [POINTER(lop_ceilings_t)]),
         "lop_quantize_blocks": (c_int, [c_void_p, c_longlong, c_void_p]),
         "lop_rowwise_f8": (c_int, [c_void_p, c_longlong, c_void_p]),
+        "lop_rowwise_f8_kernel": (c_int, [c_void_p, c_longlong, c_char_p, c_size_t]),
         "lop_head_norm_rope": (c_int, [c_void_p, c_longlong, c_void_p]),
         "lop_attention_workspace": (c_int, [c_void_p, c_longlong, POINTER(c_ulonglong)]),
         "lop_attention": (c_int, [c_void_p, c_longlong, c_void_p]),
@@ -432,6 +433,13 @@ def lop_quantize_blocks(op: lop_quantize_t, rows: Tuple[int, int], stream=None) 
 
 def lop_rowwise_f8(op: lop_rowwise_f8_t, rows: Tuple[int, int], stream=None) -> None:
     _check(_lib.lop_rowwise_f8(byref(op), _rows_word(*rows), _stream(stream)), "lop_rowwise_f8")
+
+
+def lop_rowwise_f8_kernel(op: lop_rowwise_f8_t, rows: Tuple[int, int]) -> str:
+    """Name of the kernel instance that lop_rowwise_f8 runs."""
+    buf = ctypes.create_string_buffer(128)
+    _check(_lib.lop_rowwise_f8_kernel(byref(op), _rows_word(*rows), buf, 128), "lop_rowwise_f8_kernel")
+    return buf.value.decode()
 
 
 def lop_head_norm_rope(op: lop_head_norm_rope_t, rows: Tuple[int, int], stream=None) -> None:
