@@ -376,7 +376,7 @@ typedef struct {
   int heads_q, heads_k;     /* heads_q a multiple of heads_k                                              */
   int head_dim;             /* a multiple of 8, at most 256                                               */
   int seqs;
-  int rows_q, rows_k;       /* rows of q (and out), of k (and v): all that may be touched                 */
+  int rows_q, rows_k;       /* rows of q (and out), of k (and v; at most 2^31 - 65): all that may be touched */
   int max_keys;             /* keys of the longest sequence, as far as known: decides only how the work is cut   */
   int causal;
   float scale;              /* finite, above 0                                                            */

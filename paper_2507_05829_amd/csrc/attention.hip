@@ -18,6 +18,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <climits>
 #include <cmath>
 
 #include "conv_common.hpp"
@@ -698,8 +699,9 @@ int check_sizes(const lop_attention_t* op, lop_rows_t rows) {
   if (!known_dtype(op->dtype) || op->head_dim % 8 || op->head_dim > 256) return LOP_ERR_UNSUPPORTED;
   if (op->heads_q % op->heads_k) return LOP_ERR_SHAPE;
   if (const int e = check_band(rows, op->rows_q)) return e;
+  // (numbers of packed rows and of keys, up to the end of a tile, are 32 bits)
   const long long group = op->heads_q / op->heads_k, packed = (long long)op->rows_q * group;
-  if (packed >= (1LL << 31) || (packed / kRows + op->seqs + 1) * op->heads_k > launch_blocks(256) ||
+  if (packed >= (1LL << 31) || op->rows_k > INT_MAX - 64 || (packed / kRows + op->seqs + 1) * op->heads_k > launch_blocks(256) ||
       ceil_div((long long)op->rows_q * op->heads_q, 4) > launch_blocks(256))
     return LOP_ERR_UNSUPPORTED;
   return LOP_OK;
