@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from operator_cases import HALF, U32, lse_tolerance, values
+from operator_cases import HALF, U32, attention_tolerance, lse_tolerance, values
 from oracle import transformer as plain
 from test_operators_gpu import attend
 
@@ -124,3 +124,18 @@ def test_scores_past_the_range_show(sign, max_keys, dtype):
         assert np.isnan(out[1]).all()
     else:
         near(out[1], v[n + 50].astype(np.float64), d, dtype, 1)
+
+
+@pytest.mark.parametrize("max_keys", [1, 5000])
+@pytest.mark.parametrize("power", [80, 110, 120])
+def test_operands_far_apart(power, max_keys):
+    """Queries of about 2^power against keys of about 2^-power and values of 2^power / 4: ordinary scores of operands that are anything but."""
+    rng = np.random.default_rng(7)
+    q, k, v = (values(rng, (n, 1, 64), "f32") for n in (4, 300, 300))
+    tall = [np.float32(2.0 ** power) * q, np.float32(2.0 ** -power) * k, np.float32(2.0 ** (power - 2)) * v]
+    o, b, e = [0, 3, 4], [0, 10], [300, 11]
+    out, lse = attend(*tall, o, b, e, "f32", max_keys=max_keys)
+    want, want_lse, size, spread = plain.attention(*tall, o, b, e, 0.125, True)
+    tol = attention_tolerance(want, size, spread, 300, 64, "f32")
+    assert np.isfinite(out).all() and (np.abs(out - want) <= tol).all()
+    assert (np.abs(lse - want_lse) <= lse_tolerance(want_lse, spread, 300, 64)).all()
