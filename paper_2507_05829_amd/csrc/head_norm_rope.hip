@@ -106,7 +106,17 @@ __global__ __launch_bounds__(256) void head_norm_rope_kernel(const RopeParams p)
       for (int i = 0; i < 4; ++i) sum += a[i] * a[i] + b[i] * b[i];
 #pragma unroll
       for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d, 64);
-      const float r = 1.f / sqrtf(sum * p.by_dim + p.eps);
+      float mean = sum * p.by_dim + p.eps, by = 1.f;
+      if (!(mean >= 0x1p-100f && mean <= 0x1p120f)) {   // values beyond 2^60 or below 2^-50, whose squares fp32 does not hold: of the values times a power of two
+        by = mean < 1.f ? 0x1p70f : 0x1p-70f;           // (in a loop of its own for such heads: 80 registers, prompts 99 us instead of 70)
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sum += (a[i] * by) * (a[i] * by) + (b[i] * by) * (b[i] * by);
+#pragma unroll
+        for (int d = 1; d < LANES; d *= 2) sum += __shfl_xor(sum, d, 64);
+        mean = sum * p.by_dim + p.eps * by * by;
+      }
+      const float r = by / sqrtf(mean);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         a[i] *= r * (is_k ? wk[0][i] : wq[0][i]);
