@@ -282,7 +282,8 @@ LOP_API int lop_plan_rowwise(const lop_rowwise_t* layers, int n_layers, int m, i
  * LOP_ERR_INVALID_ARG, and so are strides that let rows, heads or scales of an output overlap. Outputs do not overlap inputs unless a comment allows it. */
 
 /* A matrix in 8-bit floating point (e4m3: 3 fraction bits, largest value 448, no infinities) with a scale for each block
- * of LOP_F8_BLOCK columns: q = x * (448 / a) rounded to nearest even, scale = a / 448, a = max(|x| over the block, 2^-64).
+ * of LOP_F8_BLOCK columns: q = x * (448 / a) rounded to nearest even, scale = a / 448, a = max(|x| over the block, 2^-64); both quotients and the product are of fp32 (a value
+ * that lies halfway between two e4m3 values to 2^-22 of it may be rounded to either).
  * Activations have blocks of one row, weights of LOP_F8_BLOCK rows (block_rows). A NaN stays a NaN and
  * leaves the rest of its block as it would be without it; an infinity makes the scale infinite, itself NaN and the rest
  * of its block zero. */

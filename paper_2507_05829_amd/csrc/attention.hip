@@ -13,7 +13,7 @@
 // tile ahead. Where there are few workgroups the keys are cut into parts, and a second kernel joins their results.
 //
 // Bound: prompts by the matrix cores and the vector instructions of the weights, which one wavefront's products and the other's weights share a SIMD for: a
-// causal prompt of 8192 rows of 32 heads (8 of keys) of 128 bf16 values takes 506 us, 1.08 PFLOP/s (a large library product 1.2). Single rows
+// causal prompt of 8192 rows of 32 heads (8 of keys) of 128 bf16 values takes 502 us, 1.09 PFLOP/s (a large library product 1.2), on a slower machine 549. Single rows
 // by reading keys and values: 32 rows on caches of 2000 to 8000 keys of 8 heads of 128 bf16 values 149 us, 4.9 TB/s.
 #include <hip/hip_runtime.h>
 
