@@ -655,7 +655,7 @@ def _here():
     """The current device, its current stream, and 1 where gradients are recorded + 2 where tensors may have tangents (a level of forward-mode
     derivatives is open: then _refuse looks at every tensor)."""
     device = _current_device()
-    return device, _current_stream(device), _grad_enabled() + 2 * (_forward_ad._current_level >= 0)
+    return device, _current_stream(device), _grad_enabled() if _forward_ad._current_level < 0 else _grad_enabled() + 2
 
 
 def _no_number(e: struct.error):
@@ -688,7 +688,7 @@ def quantize_blocks(x, block_rows: int = 1, q=None, scale=None, rows=None):
     xs, qs, ss = x.stride(), q.stride(), scale.stride()
     if (q.dtype is not _F8 or scale.dtype is not torch.float32 or q.shape != shape or scale.shape != blocks
             or x.get_device() != device or q.get_device() != device or scale.get_device() != device
-            or grad > 1 or (grad and (x.requires_grad or q.requires_grad or scale.requires_grad)) or xs[1] != 1 or qs[1] != 1):
+            or (grad and (grad > 1 or x.requires_grad or q.requires_grad or scale.requires_grad)) or xs[1] != 1 or qs[1] != 1):
         _refuse(device, grad, ("x", x, x.dtype, None, 1), ("q", q, _F8, shape, 1), ("scale", scale, torch.float32, blocks, 0))
     try:
         op = _QUANTIZE.pack(m, k, code, block_rows, x.data_ptr(), xs[0], q.data_ptr(), qs[0], scale.data_ptr(), ss[0], ss[1])
@@ -719,7 +719,7 @@ def rowwise_f8(x, x_scale, w, w_scale, bias=None, act: str = "none", residual=No
             or x_scale.shape != (m, kb) or w_scale.shape != (-(-n // LOP_F8_BLOCK), kb) or y.shape != (m, n)
             or x.get_device() != device or w.get_device() != device or x_scale.get_device() != device
             or w_scale.get_device() != device or y.get_device() != device
-            or grad > 1 or (grad and (x.requires_grad or w.requires_grad or x_scale.requires_grad or w_scale.requires_grad or y.requires_grad))
+            or (grad and (grad > 1 or x.requires_grad or w.requires_grad or x_scale.requires_grad or w_scale.requires_grad or y.requires_grad))
             or xs[1] != 1 or ws[1] != 1 or ys[1] != 1):
         _refuse(device, grad, ("x", x, _F8, None, 1), ("w", w, _F8, (n, k), 1), ("x_scale", x_scale, f32, (m, kb), 0),
                 ("w_scale", w_scale, f32, (-(-n // LOP_F8_BLOCK), kb), 0), ("y", y, dtype, (m, n), 1))
@@ -754,7 +754,7 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
         q_out = torch.empty(shape, dtype=dtype, device=q.device)
     qs, qos = q.stride(), q_out.stride()
     if (q_out.dtype is not dtype or q_out.shape != shape or q.get_device() != device or q_out.get_device() != device
-            or grad > 1 or (grad and (q.requires_grad or q_out.requires_grad)) or qs[2] != 1 or qos[2] != 1):
+            or (grad and (grad > 1 or q.requires_grad or q_out.requires_grad)) or qs[2] != 1 or qos[2] != 1):
         _refuse(device, grad, ("q", q, dtype, None, 1), ("q_out", q_out, dtype, shape, 1))
     hk = k_at = k_out_at = 0
     ks = kos = (0, 0)
@@ -765,7 +765,7 @@ def head_norm_rope(q, k, positions, freq, q_weight=None, k_weight=None, eps: flo
             k_out = torch.empty(k_shape, dtype=dtype, device=q.device)
         ks, kos = k.stride(), k_out.stride()
         if (k.dtype is not dtype or k_out.dtype is not dtype or k_shape[0] != tokens or k_shape[2] != d or k_out.shape != k_shape
-                or k.get_device() != device or k_out.get_device() != device or grad > 1 or (grad and (k.requires_grad or k_out.requires_grad))
+                or k.get_device() != device or k_out.get_device() != device or (grad and (grad > 1 or k.requires_grad or k_out.requires_grad))
                 or ks[2] != 1 or kos[2] != 1):
             _refuse(device, grad, ("k", k, dtype, (tokens, hk, d), 1), ("k_out", k_out, dtype, k_shape, 1))
         k_at, k_out_at = k.data_ptr(), k_out.data_ptr()
@@ -820,7 +820,7 @@ def attention(q, k, v, q_offsets, k_begin, k_end, scale: float, causal: bool = T
             or k_end.dtype is not i32 or k_shape[2] != d or v.shape != k_shape or out.shape != shape or q_offsets.shape != (seqs + 1,)
             or k_end.shape != (seqs,) or q.get_device() != device or k.get_device() != device or v.get_device() != device
             or out.get_device() != device or q_offsets.get_device() != device or k_begin.get_device() != device
-            or k_end.get_device() != device or grad > 1 or (grad and (q.requires_grad or k.requires_grad or v.requires_grad or out.requires_grad))
+            or k_end.get_device() != device or (grad and (grad > 1 or q.requires_grad or k.requires_grad or v.requires_grad or out.requires_grad))
             or qs[2] != 1 or ks[2] != 1 or vs[2] != 1 or os_[2] != 1 or q_offsets.stride(0) != 1 or k_begin.stride(0) != 1
             or k_end.stride(0) != 1):
         _refuse(device, grad, ("q", q, dtype, None, 1), ("k", k, dtype, (rows_k, hk, d), 1), ("v", v, dtype, k_shape, 1),

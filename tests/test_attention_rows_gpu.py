@@ -5,7 +5,7 @@ import pytest
 import torch
 
 from operator_cases import TORCH, values
-from test_operators_gpu import attend, packed
+from test_operators_gpu import attend, check_attention, packed
 
 pytestmark = pytest.mark.gpu
 
@@ -54,3 +54,19 @@ def test_later_tokens_do_not_change_a_row(dtype, d):
     short = attend(q[:100], k[:100], v[:100], [0, 100], [0], [100], dtype, max_keys=1)
     long = attend(q, k, v, o, b, e, dtype, max_keys=1)
     same((long[0][:100], long[1][:, :100]), short)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_keys", [1, 5000])
+@pytest.mark.parametrize("d", [8, 72, 96, 128, 136, 256])
+def test_hidden_values_of_all_head_sizes(d, max_keys, dtype):
+    """Some rows of a workgroup go through their keys again, others not: later tokens' values are NaN or infinite, one key of the second sequence has scores
+    far from the others', one value of it is infinite, and the third sequence sees its last tile partly."""
+    rng = np.random.default_rng(d + 3)
+    q, k, v, o, b, e = packed(rng, [(70, 70), (9, 300), (130, 190)], 6, 2, d, dtype, room=320)
+    v[b[0] + 40:e[0], 0, :3] = np.nan
+    v[b[0] + 60:e[0], 1, d - 1] = np.inf
+    k[b[1] + 17] *= np.float32(2.0 ** 60)
+    v[b[1] + 299, 1] = -np.inf
+    v[b[2] + 150:e[2]:7] = np.nan
+    check_attention(attend(q, k, v, o, b, e, dtype, max_keys=max_keys), q, k, v, o, b, e, dtype)
