@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from operator_cases import TORCH, values
+from paper_2507_05829_amd import lop
 from test_operators_gpu import attend, check_attention, packed
 
 pytestmark = pytest.mark.gpu
@@ -70,3 +71,25 @@ def test_hidden_values_of_all_head_sizes(d, max_keys, dtype):
     v[b[1] + 299, 1] = -np.inf
     v[b[2] + 150:e[2]:7] = np.nan
     check_attention(attend(q, k, v, o, b, e, dtype, max_keys=max_keys), q, k, v, o, b, e, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_keys", [1, 5000])
+@pytest.mark.parametrize("d", [8, 40, 72, 120, 128, 200])
+def test_what_lies_between_rows_and_heads_is_not_read(d, max_keys, dtype):
+    """Heads of d values in places for more, NaNs behind them; and an output in such places, which keeps what is behind them."""
+    rng = np.random.default_rng(d + 4)
+    q, k, v, o, b, e = packed(rng, [(20, 150), (3, 40)], 4, 2, d, dtype)
+    plain_out, _ = attend(q, k, v, o, b, e, dtype, max_keys=max_keys)
+    dt, room = TORCH[dtype], d + 24
+
+    def inside(a):
+        t = torch.full((a.shape[0], a.shape[1], room), float("nan"), dtype=dt, device="cuda")
+        t[..., :d] = torch.from_numpy(a).cuda().to(dt)
+        return t[..., :d]
+
+    out = inside(np.zeros_like(q))
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")  # noqa: E731
+    lop.attention(inside(q), inside(k), inside(v), i32(o), i32(b), i32(e), d ** -0.5, max_keys=max_keys, out=out)
+    np.testing.assert_array_equal(out.float().cpu().numpy(), plain_out)
+    assert out.as_strided((q.shape[0], 4, 24), (4 * room, room, 1), d).isnan().all()

@@ -43,8 +43,8 @@ def check(got, want, off, dtype, what, terms=0.0):
 
 
 def wider(t, before, behind):
-    """The same values inside a buffer with more columns."""
-    buf = torch.zeros(t.shape[0], before + t.shape[1] + behind, device="cuda").to(t.dtype)
+    """The same values inside a buffer with more columns, NaNs."""
+    buf = torch.full((t.shape[0], before + t.shape[1] + behind), float("nan"), device="cuda").to(t.dtype)
     buf[:, before:before + t.shape[1]] = t
     return buf[:, before:before + t.shape[1]]
 
